@@ -439,6 +439,113 @@ int fluxmoe_paged_tensor_set_class(fluxmoe_paged_tensor* p, uint32_t layer, int 
 int fluxmoe_balanced_split(double beta_gpu, double beta_cpu, uint32_t experts_per_rank,
                            double* x_bw, uint32_t* n_down, uint32_t* n_fused);
 
+/* ------------------------------------------------------------------------------------------
+ * Around the routed experts: the router in front of them, tokens sorted by expert and back for experts that
+ * run elsewhere, the norms on either side of a block, and the gradients of all three.  Device pointers
+ * only; no context; nothing is kept between calls and nothing allocated; the calls only enqueue on
+ * `stream`, so their order with the calls above is the stream's.  T <= 2^20, E <= 4096, K <= 64, hidden <= 2^20;
+ * T = 0 is valid.  Strides are in elements, from one row to the next.  Element types are FLUXMOE_BF16 or
+ * FLUXMOE_F32; sums are FP32, and each output is rounded once.  The same call gives the same bits.
+ * Rows at 16-byte addresses (strides too) are read 16 bytes at a time; any others an element at a time.
+ * ------------------------------------------------------------------------------------------ */
+#define FLUXMOE_BF16 0u
+#define FLUXMOE_F32 1u
+
+/*
+ * Router: the K best experts of each token and their gates, as fluxmoe_expert_ffn takes them.
+ *   logits   device `type` [T][E], row_stride apart; bias device float [E] or NULL
+ *   topk_ids device int32 [T][K]; topk_w device float [T][K]
+ * Scores are the softmax over the E logits, or with FLUXMOE_ROUTE_SIGMOID each logit's 1 / (1 + e^-logit).
+ * The K largest scores (sigmoids: score + bias) are chosen and written in descending order, equal ones by
+ * ascending expert.  A gate is its expert's score without the bias, with FLUXMOE_ROUTE_RENORMALIZE divided by
+ * the sum over the chosen ones, times `scale`.
+ * An expert whose logit (or score + bias) is minus infinity or not a number is never chosen: places that stay
+ * empty get expert -1 and gate 0, a row with nothing to choose only such.  (fluxmoe_expert_ffn takes such pairs
+ * with FLUXMOE_FFN_SKIP_UNMAPPED.)
+ */
+#define FLUXMOE_ROUTE_SIGMOID 1u
+#define FLUXMOE_ROUTE_RENORMALIZE 2u
+int fluxmoe_route(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride, const float* bias,
+                  uint32_t K, float scale, uint32_t flags, int32_t* topk_ids, float* topk_w, void* stream);
+/* Its gradient: d_logits (`type` [T][E], d_row_stride apart, written whole) from d_topk_w (device float [T][K]).
+ * topk_ids as fluxmoe_route gave them (distinct in a row; others than 0..E-1 count as empty); which experts
+ * are chosen, and the bias, have no gradient. */
+int fluxmoe_route_grad(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride,
+                       const int32_t* topk_ids, uint32_t K, float scale, uint32_t flags, const float* d_topk_w,
+                       void* d_logits, uint64_t d_row_stride, void* stream);
+
+/*
+ * Tokens by expert.  Pair t * K + k is token t's k-th expert topk_ids[t][k] (device int32 [T][K]); pairs with
+ * ids outside 0..E-1 are dropped.  Expert e's pairs get consecutive rows in ascending order of the pairs:
+ *   offsets  device int32 [E + 1]: its first row, a multiple of `align` (1..1024); offsets[E] the end of all
+ *   counts   device int32 [E]: its pairs
+ *   pair_row device int32 [T][K]: a pair's row, -1 = dropped
+ *   row_pair device int32 [rows_cap]: a row's pair, -1 = none (between groups and past the last one)
+ * rows_cap must be at least fluxmoe_sorted_rows (ENOMEM); workspace device memory of
+ * fluxmoe_sort_workspace_bytes (0 for small batches), needed during the call's work only.
+ */
+uint64_t fluxmoe_sorted_rows(uint32_t T, uint32_t K, uint32_t E, uint32_t align);
+uint64_t fluxmoe_sort_workspace_bytes(uint32_t T, uint32_t K, uint32_t E);
+int fluxmoe_sort_tokens(const int32_t* topk_ids, uint32_t T, uint32_t K, uint32_t E, uint32_t align, int32_t* offsets,
+                        int32_t* counts, int32_t* pair_row, int32_t* row_pair, uint64_t rows_cap, void* workspace,
+                        uint64_t workspace_bytes, void* stream);
+/* rows[r] = x[token of row r] (both `type`), 0 in rows of no pair: all rows_cap rows are written.  Its gradient is
+ * fluxmoe_combine with topk_w NULL.  Here and below a pair_row outside 0..rows_cap-1 counts as dropped. */
+int fluxmoe_dispatch(const void* x, uint32_t type, uint32_t T, uint32_t H, uint64_t x_stride, const int32_t* pair_row,
+                     uint32_t K, const int32_t* row_pair, uint64_t rows_cap, void* rows, uint64_t rows_stride,
+                     void* stream);
+/* out[t] = sum over k of topk_w[t][k] * rows[pair_row[t][k]] in the order of k; topk_w NULL: every weight is 1; dropped
+ * pairs add nothing and their weights are not read.  flags: 0 or FLUXMOE_FFN_ACCUMULATE. */
+int fluxmoe_combine(const void* rows, uint32_t rows_type, uint64_t rows_cap, uint32_t H, uint64_t rows_stride,
+                    const int32_t* pair_row, const float* topk_w, uint32_t T, uint32_t K, void* out, uint32_t out_type,
+                    uint64_t out_stride, uint32_t flags, void* stream);
+/* Its gradients: d_rows[r] = weight * d_out[token] (`rows_type`; 0 in rows of no pair: all rows_cap rows are written)
+ * and d_topk_w[t][k] = <d_out[t], rows[its row]> (0 for dropped pairs).  d_out has `out_type`. */
+int fluxmoe_combine_grad(const void* d_out, uint32_t out_type, uint64_t d_out_stride, const void* rows,
+                         uint32_t rows_type, uint64_t rows_cap, uint32_t H, uint64_t rows_stride,
+                         const int32_t* pair_row, const int32_t* row_pair, const float* topk_w, uint32_t T, uint32_t K,
+                         void* d_rows, uint64_t d_rows_stride, float* d_topk_w, void* stream);
+
+/*
+ * The norms on either side of a block, and the residual sum between them, in one pass over the rows:
+ *   y' = y / rms(y) * w_post           (y where w_post is NULL)
+ *   r  = residual + scale * gate * y'  -> residual_out
+ *   n  = r / rms(r) * w_pre            -> normed, BF16: what the next block and fluxmoe_expert_ffn read
+ * with rms(v) = sqrt(mean(v^2) + eps).  y NULL: r is the residual itself (a block's first norm) and
+ * residual_out must be NULL.  n is taken from r before r is rounded to residual_type.
+ *   y y_type [T][hidden] (fluxmoe_expert_ffn's output: FLUXMOE_F32), residual and residual_out residual_type,
+ *   w_pre and w_post weight_type [hidden]; gate device float: NULL, [T] with FLUXMOE_NORM_GATE_TOKEN or
+ *   [hidden] with FLUXMOE_NORM_GATE_CHANNEL, its sigmoid with FLUXMOE_NORM_GATE_SIGMOID.
+ *   FLUXMOE_NORM_ZERO_CENTRED: the weights are 1 + w.
+ * residual_out may be the residual's own rows.  Strides of 0 mean `hidden`.
+ */
+#define FLUXMOE_NORM_GATE_TOKEN 1u
+#define FLUXMOE_NORM_GATE_CHANNEL 2u
+#define FLUXMOE_NORM_GATE_SIGMOID 4u
+#define FLUXMOE_NORM_ZERO_CENTRED 8u
+typedef struct {
+    uint32_t hidden;
+    uint32_t y_type, residual_type, weight_type;
+    uint32_t flags;
+    float eps, scale;
+    uint32_t reserved;                 /* 0 */
+    uint64_t y_stride, residual_stride, residual_out_stride, normed_stride;
+    uint64_t d_y_stride, d_residual_stride, d_residual_out_stride, d_normed_stride; /* gradient only */
+} fluxmoe_norm_desc;
+int fluxmoe_block_norm(const fluxmoe_norm_desc* desc, uint32_t T, const void* y, const void* residual,
+                       const float* gate, const void* w_post, const void* w_pre, void* residual_out, uint16_t* normed,
+                       void* stream);
+/* Its gradients.  residual_out as the forward call left it (y NULL: the residual); d_residual_out its gradient from
+ * elsewhere, or NULL (0); d_normed BF16.  d_residual (residual_type) and d_y (y_type) have the rows of theirs;
+ * d_gate, d_w_post, d_w_pre are float, overwritten, and summed over what the gate and the weights were spread over.
+ * d_y, d_gate and d_w_post are given where y, gate and w_post are.  d_residual may be d_residual_out's own rows, d_y
+ * those of y.  workspace: device, 16-byte aligned, fluxmoe_block_norm_grad_workspace_bytes. */
+uint64_t fluxmoe_block_norm_grad_workspace_bytes(uint32_t T, uint32_t hidden);
+int fluxmoe_block_norm_grad(const fluxmoe_norm_desc* desc, uint32_t T, const void* y, const void* residual_out,
+                            const float* gate, const void* w_post, const void* w_pre, const void* d_residual_out,
+                            const uint16_t* d_normed, void* d_residual, void* d_y, float* d_gate, float* d_w_post,
+                            float* d_w_pre, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* Synchronous: read and clear the device error word (0 = none; bit 0 a block failed
  * validation during decode and was skipped, bit 1 an unmapped expert was routed to). */
 int fluxmoe_device_errors(fluxmoe_ctx* ctx, uint32_t* out_flags);

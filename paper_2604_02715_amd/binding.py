@@ -66,6 +66,18 @@ class PagedTensorInfo(C.Structure):
                 ("pad_bytes", C.c_uint64), ("n_uncompressed", C.c_uint32), ("n_pageable", C.c_uint32)]
 
 
+class NormDesc(C.Structure):
+    _fields_ = ([(n, C.c_uint32) for n in ("hidden", "y_type", "residual_type", "weight_type", "flags")]
+                + [("eps", C.c_float), ("scale", C.c_float), ("reserved", C.c_uint32)]
+                + [(n, C.c_uint64) for n in ("y_stride", "residual_stride", "residual_out_stride", "normed_stride",
+                                             "d_y_stride", "d_residual_stride", "d_residual_out_stride",
+                                             "d_normed_stride")])
+
+
+BF16, F32 = 0, 1
+ROUTE_SIGMOID, ROUTE_RENORMALIZE = 1, 2
+NORM_GATE_TOKEN, NORM_GATE_CHANNEL, NORM_GATE_SIGMOID, NORM_ZERO_CENTRED = 1, 2, 4, 8
+
 PLAN_KEEP, PLAN_RECLAIM, PLAN_RESTORE, PLAN_SKIP, PLAN_DONE = 0, 1, -1, 2, 3
 
 EXPORTS = {
@@ -104,6 +116,28 @@ EXPORTS = {
                                             C.c_void_p]),
     "fluxmoe_shared_expert_ffn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
                                             C.c_void_p, C.c_uint32, C.c_void_p]),
+    "fluxmoe_route": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint32,
+                                C.c_float, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "fluxmoe_route_grad": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint64, C.c_void_p,
+                                     C.c_uint32, C.c_float, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint64,
+                                     C.c_void_p]),
+    "fluxmoe_sorted_rows": (C.c_uint64, [C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32]),
+    "fluxmoe_sort_workspace_bytes": (C.c_uint64, [C.c_uint32, C.c_uint32, C.c_uint32]),
+    "fluxmoe_sort_tokens": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64,
+                                      C.c_void_p]),
+    "fluxmoe_dispatch": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint32,
+                                   C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "fluxmoe_combine": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint64, C.c_void_p, C.c_void_p,
+                                  C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint32,
+                                  C.c_void_p]),
+    "fluxmoe_combine_grad": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint32, C.c_uint64,
+                                       C.c_uint32, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
+                                       C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
+    "fluxmoe_block_norm": (C.c_int, [C.POINTER(NormDesc), C.c_uint32] + [C.c_void_p] * 8),
+    "fluxmoe_block_norm_grad_workspace_bytes": (C.c_uint64, [C.c_uint32, C.c_uint32]),
+    "fluxmoe_block_norm_grad": (C.c_int, [C.POINTER(NormDesc), C.c_uint32] + [C.c_void_p] * 13
+                                + [C.c_uint64, C.c_void_p]),
     "fluxmoe_stream_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p]),
     "fluxmoe_stream_mix": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_uint32, C.c_uint32,
                                      C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64), C.c_void_p]),
@@ -284,6 +318,71 @@ def fluxmoe_expert_ffn_static(ctx, layer, tokens_ptr, T, topk_ids_ptr, topk_w_pt
 
 def fluxmoe_shared_expert_ffn(ctx, w13_ptr, w2_ptr, tokens_ptr, T, out_ptr, flags=0, stream=None):
     _check(lib().fluxmoe_shared_expert_ffn(ctx, w13_ptr, w2_ptr, tokens_ptr, T, out_ptr, flags, stream))
+
+
+# ---------------------------------------------------------------------- around the routed experts
+def fluxmoe_route(logits_ptr, type_, T, E, row_stride, bias_ptr, K, scale, flags, topk_ids_ptr, topk_w_ptr,
+                  stream=None):
+    _check(lib().fluxmoe_route(logits_ptr, type_, T, E, row_stride, bias_ptr, K, scale, flags, topk_ids_ptr,
+                               topk_w_ptr, stream))
+
+
+def fluxmoe_route_grad(logits_ptr, type_, T, E, row_stride, topk_ids_ptr, K, scale, flags, d_topk_w_ptr,
+                       d_logits_ptr, d_row_stride, stream=None):
+    _check(lib().fluxmoe_route_grad(logits_ptr, type_, T, E, row_stride, topk_ids_ptr, K, scale, flags, d_topk_w_ptr,
+                                    d_logits_ptr, d_row_stride, stream))
+
+
+def fluxmoe_sorted_rows(T, K, E, align=1) -> int:
+    return int(lib().fluxmoe_sorted_rows(T, K, E, align))
+
+
+def fluxmoe_sort_workspace_bytes(T, K, E) -> int:
+    return int(lib().fluxmoe_sort_workspace_bytes(T, K, E))
+
+
+def fluxmoe_sort_tokens(topk_ids_ptr, T, K, E, align, offsets_ptr, counts_ptr, pair_row_ptr, row_pair_ptr, rows_cap,
+                        workspace_ptr, workspace_bytes, stream=None):
+    _check(lib().fluxmoe_sort_tokens(topk_ids_ptr, T, K, E, align, offsets_ptr, counts_ptr, pair_row_ptr,
+                                     row_pair_ptr, rows_cap, workspace_ptr, workspace_bytes, stream))
+
+
+def fluxmoe_dispatch(x_ptr, type_, T, H, x_stride, pair_row_ptr, K, row_pair_ptr, rows_cap, rows_ptr, rows_stride,
+                     stream=None):
+    _check(lib().fluxmoe_dispatch(x_ptr, type_, T, H, x_stride, pair_row_ptr, K, row_pair_ptr, rows_cap, rows_ptr,
+                                  rows_stride, stream))
+
+
+def fluxmoe_combine(rows_ptr, rows_type, rows_cap, H, rows_stride, pair_row_ptr, topk_w_ptr, T, K, out_ptr, out_type,
+                    out_stride, flags=0, stream=None):
+    _check(lib().fluxmoe_combine(rows_ptr, rows_type, rows_cap, H, rows_stride, pair_row_ptr, topk_w_ptr, T, K,
+                                 out_ptr, out_type, out_stride, flags, stream))
+
+
+def fluxmoe_combine_grad(d_out_ptr, out_type, d_out_stride, rows_ptr, rows_type, rows_cap, H, rows_stride,
+                         pair_row_ptr, row_pair_ptr, topk_w_ptr, T, K, d_rows_ptr, d_rows_stride, d_topk_w_ptr,
+                         stream=None):
+    _check(lib().fluxmoe_combine_grad(d_out_ptr, out_type, d_out_stride, rows_ptr, rows_type, rows_cap, H, rows_stride,
+                                      pair_row_ptr, row_pair_ptr, topk_w_ptr, T, K, d_rows_ptr, d_rows_stride,
+                                      d_topk_w_ptr, stream))
+
+
+def fluxmoe_block_norm(desc, T, y_ptr, residual_ptr, gate_ptr, w_post_ptr, w_pre_ptr, residual_out_ptr, normed_ptr,
+                       stream=None):
+    _check(lib().fluxmoe_block_norm(desc, T, y_ptr, residual_ptr, gate_ptr, w_post_ptr, w_pre_ptr, residual_out_ptr,
+                                    normed_ptr, stream))
+
+
+def fluxmoe_block_norm_grad_workspace_bytes(T, hidden) -> int:
+    return int(lib().fluxmoe_block_norm_grad_workspace_bytes(T, hidden))
+
+
+def fluxmoe_block_norm_grad(desc, T, y_ptr, residual_out_ptr, gate_ptr, w_post_ptr, w_pre_ptr, d_residual_out_ptr,
+                            d_normed_ptr, d_residual_ptr, d_y_ptr, d_gate_ptr, d_w_post_ptr, d_w_pre_ptr,
+                            workspace_ptr, workspace_bytes, stream=None):
+    _check(lib().fluxmoe_block_norm_grad(desc, T, y_ptr, residual_out_ptr, gate_ptr, w_post_ptr, w_pre_ptr,
+                                         d_residual_out_ptr, d_normed_ptr, d_residual_ptr, d_y_ptr, d_gate_ptr,
+                                         d_w_post_ptr, d_w_pre_ptr, workspace_ptr, workspace_bytes, stream))
 
 
 def fluxmoe_stream_copy(dst_ptr, src_ptr, nbytes, n_workgroups, stream=None):

@@ -37,13 +37,6 @@ int set_error(int status, const char* fmt, ...) {
 
 using namespace fluxmoe;
 
-#define HIPCHECK(call)                                                                  \
-    do {                                                                                \
-        hipError_t e_ = (call);                                                         \
-        if (e_ != hipSuccess)                                                           \
-            return set_error(FLUXMOE_EHIP, "%s failed: %s", #call, hipGetErrorString(e_)); \
-    } while (0)
-
 namespace {
 constexpr int kRing = 4;
 // Events between kernels of this device: no fence towards the host and other devices, which holds the stream for another

@@ -9,6 +9,13 @@
 #include "fluxmoe.h"
 #include "kernels.h"
 
+#define HIPCHECK(call)                                                                  \
+    do {                                                                                \
+        hipError_t e_ = (call);                                                         \
+        if (e_ != hipSuccess)                                                           \
+            return set_error(FLUXMOE_EHIP, "%s failed: %s", #call, hipGetErrorString(e_)); \
+    } while (0)
+
 namespace fluxmoe {
 
 int set_error(int status, const char* fmt, ...);

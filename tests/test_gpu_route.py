@@ -1,0 +1,236 @@
+"""fluxmoe_route and fluxmoe_route_grad against plain forms in 64 bits: choice, order and ties of the experts, gates, gradients
+(by the formula and by differences), rows that masks leave empty, infinities, strides that are not aligned.
+
+Tolerances: u = 2^-24.  A gate is e^(l - m) over a sum: l - m is rounded (relative error of the power |l - m| u), expf is good to
+2 ulp, sum and division add log2(E) + 8 roundings at most; so (|l - m| + log2(E) + 16) u of the gate, and the same of the
+gradient's largest term in the row, three times over (products, the mean over the gates, the difference).  A chosen sigmoid's
+score is off by 4 u at most, so a choice may differ from that in 64 bits only where two scores are nearer than 16 u."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_02715_amd import moe_block as M
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+BF16 = 2.0 ** -8                # a BF16 output's rounding, with room for a tie that falls the other way
+
+
+def make_logits(T, E, dtype, seed, spread=1.5):
+    g = torch.Generator().manual_seed(seed)
+    return (spread * torch.randn(T, E, generator=g)).to(dtype)
+
+
+def plain_keys(logits, bias, score):
+    """what the choice goes by, in 64 bits; minus infinity where an expert cannot be chosen"""
+    l = logits.double()
+    key = l if score == "softmax" else torch.sigmoid(l) + (0.0 if bias is None else bias.double())
+    return torch.where(torch.isnan(key) | torch.isnan(l) | (l == -math.inf), -math.inf, key)
+
+
+def plain_gates(logits, ids, score, renormalize, scale):
+    l = torch.where(torch.isnan(logits), -math.inf, logits).double()
+    p = torch.sigmoid(l) if score == "sigmoid" else torch.softmax(l, dim=1).nan_to_num(0.0)
+    p = torch.where(ids >= 0, torch.gather(p, 1, ids.clamp(min=0)), 0.0)
+    if renormalize:
+        p = p / p.sum(dim=1, keepdim=True).clamp(min=1e-300)
+    return p * scale
+
+
+def run(logits, K, bias=None, **kw):
+    T = logits.shape[0]
+    ids = torch.full((T, K), -7, dtype=torch.int32, device="cuda")
+    gates = torch.full((T, K), math.nan, device="cuda")
+    M.route(logits, ids, gates, bias=None if bias is None else bias.cuda(), **kw)
+    torch.cuda.synchronize()
+    return ids.cpu().long(), gates.cpu()
+
+
+def check(logits_cpu, logits_gpu, K, score, renormalize, scale=1.0, bias=None):
+    E = logits_cpu.shape[1]
+    ids, gates = run(logits_gpu, K, bias, score=score, renormalize=renormalize, scale=scale)
+    key = plain_keys(logits_cpu, bias, score)
+    order = torch.sort(key, dim=1, descending=True, stable=True)
+    want = torch.where(order.values[:, :K] > -math.inf, order.indices[:, :K], -1)
+    if score == "softmax":
+        assert torch.equal(ids, want)
+    else:
+        assert torch.equal(ids < 0, want < 0)
+        got = torch.gather(key, 1, ids.clamp(min=0))
+        near = (got - order.values[:, :K]).abs() <= 16 * U
+        assert bool((near | (ids < 0)).all()), "a chosen expert is not among the best"
+        live = [row[row >= 0] for row in ids]
+        assert all(row.unique().numel() == row.numel() for row in live)
+    exact = plain_gates(logits_cpu, ids, score, renormalize, scale)
+    l = torch.where(torch.isfinite(logits_cpu.float()), logits_cpu.float(), 0.0)
+    spread = float((l.max() - l.min()).abs()) if l.numel() else 0.0
+    tol = (min(spread, 104.0) + math.log2(E) + 16) * U
+    assert bool(((gates.double() - exact).abs() <= tol * exact.abs() + 2.0 ** -126).all())
+    return ids
+
+
+@pytest.mark.parametrize("E,K", [(1, 1), (2, 2), (8, 2), (8, 8), (16, 2), (16, 16), (17, 3), (64, 8), (64, 9), (65, 8), (160, 8), (256, 33),
+                                 (257, 10), (512, 10), (512, 64), (513, 10), (1000, 12), (1025, 10), (2048, 8), (2049, 5), (4096, 64)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_choice_and_gates(E, K, dtype):
+    for T in (1, 7, 131):
+        logits = make_logits(T, E, dtype, 1000 * E + K + T)
+        bias = (torch.randn(E, generator=torch.Generator().manual_seed(E)) * 30).round() * 0.001
+        dev = logits.cuda()
+        for renormalize in (True, False):
+            check(logits, dev, K, "softmax", renormalize)
+            check(logits, dev, K, "sigmoid", renormalize, scale=2.5, bias=bias)
+        check(logits, dev, K, "sigmoid", True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E", [8, 160, 512, 700])
+def test_equal_scores_go_to_the_lowest_expert(E, dtype):
+    logits = make_logits(64, E, torch.float32, 5).mul(2).round().div(2).to(dtype)       # few distinct values
+    logits[0] = 0.0
+    logits[1, ::2] = -0.0                                                              # equal to the zeros between them
+    logits[1, 1::2] = 0.0
+    K = min(E, 10)
+    ids = check(logits, logits.cuda(), K, "softmax", True)
+    assert ids[0].tolist() == list(range(K)) and ids[1].tolist() == list(range(K))
+    ids = run(logits.cuda(), K, score="sigmoid", renormalize=False)[0]
+    assert ids[0].tolist() == list(range(K)) and ids[1].tolist() == list(range(K))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("E,K", [(8, 2), (40, 6), (160, 8), (512, 10), (600, 10)])
+def test_masks_infinities_and_nan(E, K, score, renormalize):
+    logits = make_logits(12, E, torch.float32, 9)
+    lowest = torch.finfo(torch.float32).min
+    logits[0] = -math.inf                                    # nothing to choose
+    logits[1] = -math.inf
+    logits[1, E // 2] = 0.3                                  # one expert
+    logits[2] = lowest                                       # masks of the type's lowest value are numbers like others
+    logits[3] = lowest
+    logits[3, E - 1] = 1.0
+    logits[4, ::2] = math.nan
+    logits[5] = math.nan
+    logits[6, 1::2] = -math.inf
+    logits[7] = 200.0
+    logits[8] = -200.0                                       # sigmoids below the smallest float: no gates, no division by 0
+    logits[9, 0], logits[9, 1:] = 3.0e38, -3.0e38
+    ids, gates = run(logits.cuda(), K, score=score, renormalize=renormalize)
+    assert bool(torch.isfinite(gates).all())
+    key = plain_keys(logits, None, score)
+    free = (key > -math.inf).sum(dim=1).clamp(max=K)
+    assert torch.equal((ids >= 0).sum(dim=1), free)
+    assert bool(((ids >= 0) | (gates == 0)).all())
+    assert ids[0].tolist() == [-1] * K and ids[5].tolist() == [-1] * K
+    assert int(ids[1, 0]) == E // 2
+    if score == "softmax":
+        assert ids[2].tolist() == list(range(K)) and int(ids[3, 0]) == E - 1 and ids[7].tolist() == list(range(K))
+        assert abs(float(gates[2].sum()) - (1.0 if renormalize else K / E)) < 1e-6
+        assert abs(float(gates[3, 0]) - 1.0) < 1e-6 and float(gates[3, 1:].abs().sum()) == 0.0
+    rows = [1, 4, 6, 7, 10, 11]
+    check(logits[rows], logits[rows].cuda(), K, score, renormalize)
+
+
+def test_an_infinite_logit_takes_the_whole_softmax():
+    logits = make_logits(3, 40, torch.float32, 2)
+    logits[0, 7] = math.inf
+    logits[1, 7] = logits[1, 3] = math.inf
+    for renormalize in (True, False):
+        ids, gates = run(logits.cuda(), 4, renormalize=renormalize)
+        assert int(ids[0, 0]) == 7 and gates[0].tolist() == [1.0, 0.0, 0.0, 0.0]
+        assert ids[1, :2].tolist() == [3, 7] and gates[1].tolist() == [0.5, 0.5, 0.0, 0.0]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E", [8, 160, 509, 512])
+def test_strides_and_alignment(E, dtype):
+    wide = make_logits(33, E + 13, dtype, 3)
+    dev = wide.cuda()
+    for at in (0, 1, 8):                                     # rows that start at 16 bytes, and rows that do not
+        check(wide[:, at:at + E].contiguous(), dev[:, at:at + E], min(E, 8), "softmax", False)
+        logits = dev[:, at:at + E]
+        ids, _ = run(logits, min(E, 8))
+        d_gates = torch.randn(33, min(E, 8), device="cuda")
+        one, two = torch.empty(33, E, dtype=dtype, device="cuda"), torch.full((33, E + 13), 5.0, dtype=dtype, device="cuda")
+        M.route_grad(logits.contiguous(), ids.int().cuda(), d_gates, one, renormalize=False)
+        M.route_grad(logits, ids.int().cuda(), d_gates, two[:, at:at + E], renormalize=False)
+        assert torch.equal(one, two[:, at:at + E])
+        assert bool((two[:, :at] == 5.0).all()) and bool((two[:, at + E:] == 5.0).all())
+
+
+def grad_64(logits, ids, d_gates, score, renormalize, scale):
+    l = logits.double().requires_grad_(True)
+    p = torch.sigmoid(l) if score == "sigmoid" else torch.softmax(l, dim=1)
+    p = torch.where(ids >= 0, torch.gather(p, 1, ids.clamp(min=0)), 0.0)
+    if renormalize:
+        p = p / p.sum(dim=1, keepdim=True).clamp(min=1e-300)
+    (p * scale * d_gates.double()).sum().backward()
+    return l.grad
+
+
+@pytest.mark.parametrize("E,K", [(2, 1), (8, 2), (16, 16), (17, 3), (64, 8), (160, 8), (300, 40), (512, 10), (513, 10), (1500, 16), (4096, 64)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_gradient_against_the_formula(E, K, dtype, score, renormalize):
+    for T in (1, 77):
+        logits = make_logits(T, E, dtype, E + T)
+        if E > 2 * K:
+            logits[:, E // 3] = -math.inf
+        ids, _ = run(logits.cuda(), K, score=score, renormalize=renormalize)
+        if K > 2 and T > 1:
+            ids[5, 1] = -1                                   # a pair that something else dropped
+        d_gates = torch.randn(T, K, generator=torch.Generator().manual_seed(K))
+        got = torch.full((T, E), math.nan, dtype=dtype, device="cuda")
+        M.route_grad(logits.cuda(), ids.int().cuda(), d_gates.cuda(), got, scale=2.5, score=score, renormalize=renormalize)
+        want = grad_64(logits, ids, d_gates, score, renormalize, 2.5)
+        want = torch.where(logits == -math.inf, 0.0, want)
+        # the largest term of a row: a score (at most 1, or its share) times scale times the largest d gate
+        l = torch.where(torch.isfinite(logits.float()), logits.float(), 0.0)
+        term = 2.5 * d_gates.abs().amax(dim=1, keepdim=True).double()
+        tol = 3 * (float(l.max() - l.min()) + math.log2(E) + 16) * U * term
+        if dtype == torch.bfloat16:
+            tol = tol + BF16 * want.abs()
+        assert bool(((got.cpu().double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_gradient_against_differences(score, renormalize):
+    T, E, K, h = 4, 24, 5, 1e-4
+    logits = make_logits(T, E, torch.float32, 77)
+    ids, _ = run(logits.cuda(), K, score=score, renormalize=renormalize)
+    d_gates = torch.randn(T, K, generator=torch.Generator().manual_seed(1))
+    got = torch.empty(T, E, device="cuda")
+    M.route_grad(logits.cuda(), ids.int().cuda(), d_gates.cuda(), got, score=score, renormalize=renormalize)
+    value = lambda l: (plain_gates(l, ids, score, renormalize, 1.0) * d_gates.double()).sum(dim=1)
+    for e in range(E):
+        step = torch.zeros(T, E, dtype=torch.float64)
+        step[:, e] = h
+        slope = (value(logits.double() + step) - value(logits.double() - step)) / (2 * h)
+        # a third derivative of a score is at most 1, so the difference is off by K h^2 |d gate|; the kernel by 3 * 32 u |d gate|
+        tol = (K * h * h + 96 * U) * float(d_gates.abs().max())
+        assert bool(((got[:, e].cpu().double() - slope).abs() <= tol).all())
+
+
+def test_no_tokens_and_an_expert_out_of_range():
+    empty = torch.empty(0, 8, device="cuda")
+    M.route(empty, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))
+    M.route_grad(empty, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"), torch.empty(0, 8, device="cuda"))
+    logits = make_logits(1, 8, torch.float32, 0).cuda()
+    d = torch.full((1, 8), math.nan, device="cuda")
+    M.route_grad(logits, torch.tensor([[8, -3]], dtype=torch.int32, device="cuda"), torch.ones(1, 2, device="cuda"), d, renormalize=False)
+    assert d.abs().sum().item() == 0.0
+
+
+def test_on_another_stream_and_again():
+    logits = make_logits(3000, 512, torch.bfloat16, 8).cuda()
+    ids, gates = run(logits, 10)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = [torch.empty(3000, 10, dtype=torch.int32, device="cuda"), torch.empty(3000, 10, device="cuda")]
+    for _ in range(3):
+        M.route(logits, *other, stream=side)
+        side.synchronize()
+        assert torch.equal(other[0].cpu().long(), ids) and torch.equal(other[1].cpu(), gates)
