@@ -309,7 +309,7 @@ int fluxmoe_block_norm(const fluxmoe_norm_desc* d, uint32_t T, const void* y, co
 }
 
 uint64_t fluxmoe_block_norm_grad_workspace_bytes(uint32_t T, uint32_t H) {
-    return uint64_t(norm_grad_partials(T, H)) * H * 3 * sizeof(float);
+    return uint64_t(norm_grad_partials(T, H)) * H * 2 * sizeof(float);
 }
 
 int fluxmoe_block_norm_grad(const fluxmoe_norm_desc* d, uint32_t T, const void* y, const void* residual_out, const float* gate,

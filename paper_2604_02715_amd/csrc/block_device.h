@@ -66,55 +66,97 @@ __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ void from_float(bf16_t* p, float v) { p->bits = uint16_t(pack_bf16_rne(v, v)); }
 __device__ __forceinline__ void from_float(float* p, float v) { *p = v; }
 
-// Eight consecutive elements in registers, as loaded: 16 bytes of BF16, 32 of FP32.
+// A row in memory, for the wavefront as a whole: reads past its columns give 0 and writes there do nothing, and a row of no
+// columns takes the place of one that is not there.  So the kernels below have no branches around their loads and stores, and a
+// wait for a load counts exactly what was issued behind it.
+typedef __amdgpu_buffer_rsrc_t row_t;
 template <typename T>
-struct Pack8;
+__device__ __forceinline__ row_t row_at(const T* base, uint64_t row, uint64_t stride, uint32_t columns) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base + row * stride), 0, int(columns * sizeof(T)), 0x00020000);
+}
+constexpr int kCached = 0, kStream = 2;      // cache policies: the usual one; touched once (non-temporal)
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// N consecutive elements in registers, as loaded.  arrive() is the place where a load has to be complete: ahead of stores, as a
+// later wait for it would be one for them, too (loads and stores count down one counter, in the order of their issue).
+template <typename T, int N>
+struct Pack;
 template <>
-struct Pack8<bf16_t> {
-    uint4 v;
-    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void load_stream(const bf16_t* p) { v = load_stream16(p); }
-    __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ float operator[](int i) const {
-        const uint32_t w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
-        return __uint_as_float((i & 1) ? (w & 0xFFFF0000u) : (w << 16));
-    }
+struct Pack<bf16_t, 8> {
+    u32x4 v;
+    template <int POLICY>
+    __device__ __forceinline__ void load(row_t row, uint32_t c) { v = __builtin_amdgcn_raw_buffer_load_b128(row, c * 2, 0, POLICY); }
+    __device__ __forceinline__ void arrive() { asm volatile("" : "+v"(v)); }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float((i & 1) ? (v[i / 2] & 0xFFFF0000u) : (v[i / 2] << 16)); }
 };
 template <>
-struct Pack8<float> {
-    uint4 lo, hi;
-    __device__ __forceinline__ void load(const float* p) {
-        lo = *reinterpret_cast<const uint4*>(p);
-        hi = *reinterpret_cast<const uint4*>(p + 4);
+struct Pack<bf16_t, 4> {
+    u32x2 v;
+    template <int POLICY>
+    __device__ __forceinline__ void load(row_t row, uint32_t c) { v = __builtin_amdgcn_raw_buffer_load_b64(row, c * 2, 0, POLICY); }
+    __device__ __forceinline__ void arrive() { asm volatile("" : "+v"(v)); }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float((i & 1) ? (v[i / 2] & 0xFFFF0000u) : (v[i / 2] << 16)); }
+};
+template <>
+struct Pack<float, 4> {
+    u32x4 v;
+    template <int POLICY>
+    __device__ __forceinline__ void load(row_t row, uint32_t c) { v = __builtin_amdgcn_raw_buffer_load_b128(row, c * 4, 0, POLICY); }
+    __device__ __forceinline__ void arrive() { asm volatile("" : "+v"(v)); }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(v[i]); }
+};
+template <>
+struct Pack<float, 8> {
+    Pack<float, 4> lo, hi;
+    template <int POLICY>
+    __device__ __forceinline__ void load(row_t row, uint32_t c) {
+        lo.load<POLICY>(row, c);
+        hi.load<POLICY>(row, c + 4);
     }
-    __device__ __forceinline__ void load_stream(const float* p) {
-        lo = load_stream16(p);
-        hi = load_stream16(p + 4);
-    }
-    __device__ __forceinline__ void zero() { lo = hi = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ float operator[](int i) const {
-        const uint4& q = i < 4 ? lo : hi;
-        const uint32_t w = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
-        return __uint_as_float(w);
-    }
+    __device__ __forceinline__ void arrive() { lo.arrive(); hi.arrive(); }
+    __device__ __forceinline__ float operator[](int i) const { return i < 4 ? lo[i] : hi[i - 4]; }
 };
 
-__device__ __forceinline__ uint4 pack8_bf16(const float (&f)[8]) {
-    return make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7]));
-}
-__device__ __forceinline__ void store8(bf16_t* p, const float (&f)[8]) { *reinterpret_cast<uint4*>(p) = pack8_bf16(f); }
-__device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
-__device__ __forceinline__ void store8_stream(bf16_t* p, const float (&f)[8]) { store_stream16(p, pack8_bf16(f)); }
-__device__ __forceinline__ void store8_stream(float* p, const float (&f)[8]) {
-    store_stream16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
-    store_stream16(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
+// N values rounded to the row's type and written from column c on.
+template <typename T, int N, int POLICY>
+__device__ __forceinline__ void store(row_t row, uint32_t c, const float* f) {
+    static_assert(N % 4 == 0, "pieces of four columns");
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const u32x4 v = {__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])};
+            __builtin_amdgcn_raw_buffer_store_b128(v, row, (c + i) * 4, 0, POLICY);
+        }
+    } else if constexpr (N == 8) {
+        const u32x4 v = {pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7])};
+        __builtin_amdgcn_raw_buffer_store_b128(v, row, c * 2, 0, POLICY);
+    } else {
+        const u32x2 v = {pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3])};
+        __builtin_amdgcn_raw_buffer_store_b64(v, row, c * 2, 0, POLICY);
+    }
 }
 
-// 1 / (1 + e^-v), each step rounded as written (the choice of experts goes by these bits)
-__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
+// An element that the whole wavefront reads and nothing in the launch writes: through the scalar cache, so that the wait for it
+// is not a wait for the vector loads and stores that are under way.
+template <typename T>
+__device__ __forceinline__ T scalar_at(const T* p, uint64_t i) {
+    return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[i];
+}
+
+// What a lane loads at once of rows of types A and B: eight columns where both are BF16, four where one is FP32.
+template <typename A, typename B>
+constexpr int kPiece = sizeof(A) == 2 && sizeof(B) == 2 ? 8 : 4;
+
+// 1 / (1 + e^-v), each step rounded as written (the choice of experts goes by these bits).  The quotient by one Newton step on
+// the hardware's reciprocal (Markstein 1990): equal to the division for every significand of the divisor, which the tests go
+// through; where the result leaves the normal numbers, the division itself.
+__device__ __forceinline__ float sigmoid(float v) {
+    const float d = 1.0f + expf(-v);
+    if (d > 0x1p100f) return 1.0f / d;
+    const float r = __builtin_amdgcn_rcpf(d);
+    return fmaf(fmaf(-d, r, 1.0f), r, r);
+}
 
 // Row kernels: `waves` wavefronts to a row of eight elements per lane, and so many rows that a workgroup has four wavefronts
 // where a row needs fewer.

@@ -87,7 +87,7 @@ struct NormArgs {
     float* d_gate;
     float* d_w_pre;
     float* d_w_post;
-    float* partials;             // [sums][n_partials][H]: w_pre, then w_post, then the channel gate, where there are such
+    float* partials;             // [sums][n_partials][H]: for w_pre, then for w_post and a channel's gate
     uint64_t d_residual_out_stride, d_normed_stride, d_residual_stride, d_y_stride;
     uint32_t n_partials;
 };

@@ -1,6 +1,7 @@
 // Tokens by expert and back: the (token, k) pairs sorted by expert, the tokens' rows copied into that order, the experts' rows
 // added up by token, and the gradient of that sum.
 #include <algorithm>
+#include <type_traits>
 
 #include "block_device.h"
 #include "block_ops.h"
@@ -68,20 +69,24 @@ __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* scratch
 }
 
 // From the experts' counts: where their rows begin (each at a multiple of align), the rows of no pair marked.  The whole
-// workgroup calls it; start[e] receives the first row of expert e.
-__device__ __forceinline__ void place_experts(const SortArgs& a, const uint32_t* count, uint32_t* start, uint32_t* scratch) {
+// workgroup calls it; start[e] holds expert e's count and receives its first row.  Only the workgroup that is asked to writes what
+// the caller gets.
+__device__ __forceinline__ void place_experts(const SortArgs& a, uint32_t* start, uint32_t* scratch, bool write) {
     const uint32_t per = (a.E + blockDim.x - 1) / blockDim.x, e0 = threadIdx.x * per;
     uint32_t sum = 0, total;
-    for (uint32_t e = e0; e < min(e0 + per, a.E); ++e) sum += (count[e] + a.align - 1) / a.align * a.align;
+    for (uint32_t e = e0; e < min(e0 + per, a.E); ++e) sum += (start[e] + a.align - 1) / a.align * a.align;
     uint32_t at = exclusive_scan(sum, scratch, total);
     for (uint32_t e = e0; e < min(e0 + per, a.E); ++e) {
-        const uint32_t n = count[e], padded = (n + a.align - 1) / a.align * a.align;
+        const uint32_t n = start[e], padded = (n + a.align - 1) / a.align * a.align;
         start[e] = at;
-        a.offsets[e] = int32_t(at);
-        a.counts[e] = int32_t(n);
-        for (uint32_t r = at + n; r < at + padded; ++r) a.row_pair[r] = -1;
+        if (write) {
+            a.offsets[e] = int32_t(at);
+            a.counts[e] = int32_t(n);
+            for (uint32_t r = at + n; r < at + padded; ++r) a.row_pair[r] = -1;
+        }
         at += padded;
     }
+    if (!write) return;
     if (threadIdx.x == 0) a.offsets[a.E] = int32_t(total);
     for (uint32_t r = total + threadIdx.x; r < a.cap; r += blockDim.x) a.row_pair[r] = -1;
 }
@@ -103,20 +108,20 @@ __device__ __forceinline__ void write_pairs(const SortArgs& a, uint32_t first, u
 // The wavefronts' counts become the number of pairs in the wavefronts before; returns the expert's sum.
 template <int WAVES>
 __device__ __forceinline__ uint32_t over_waves(uint16_t* hist, uint32_t E, uint32_t e) {
-    uint32_t n = 0;
+    uint32_t c[WAVES], n = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) c[w] = hist[w * E + e];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        const uint32_t c = hist[w * E + e];
         hist[w * E + e] = uint16_t(n);
-        n += c;
+        n += c[w];
     }
     return n;
 }
 
-// LDS of a sort workgroup: the wavefronts' counts and the experts' first rows; with all pairs in one, the experts' counts and
-// the scratch of the scan, too
-uint32_t place_lds_bytes(uint32_t waves, uint32_t E) { return (waves * E * 2 + 3) / 4 * 4 + E * 4; }
-uint32_t sort_one_lds_bytes(uint32_t waves, uint32_t E) { return place_lds_bytes(waves, E) + E * 4 + 64; }
+// LDS of a sort workgroup: the wavefronts' counts, `words` for each expert, the scratch of the scan.  48 KiB at most (2048 experts,
+// 8 wavefronts, 2 words).
+uint32_t sort_lds_bytes(uint32_t waves, uint32_t E, uint32_t words) { return (waves * E * 2 + 3) / 4 * 4 + words * E * 4 + 64; }
 
 // All pairs in one workgroup: one launch for decode batches.
 template <int WAVES, int GROUPS>
@@ -124,8 +129,7 @@ __global__ __launch_bounds__(WAVES * 64) void sort_one_kernel(SortArgs a) {
     extern __shared__ __align__(16) uint32_t lds[];
     uint16_t* hist = reinterpret_cast<uint16_t*>(lds);
     uint32_t* start = lds + (WAVES * a.E * 2 + 3) / 4;
-    uint32_t* count = start + a.E;
-    uint32_t* scratch = count + a.E;
+    uint32_t* scratch = start + a.E;
     const uint32_t wave = threadIdx.x >> 6;
     for (uint32_t i = threadIdx.x; i < (WAVES * a.E + 1) / 2; i += WAVES * 64) lds[i] = 0;
     __syncthreads();
@@ -133,9 +137,9 @@ __global__ __launch_bounds__(WAVES * 64) void sort_one_kernel(SortArgs a) {
     uint32_t rank[GROUPS];
     rank_pairs<GROUPS>(a.ids, wave * 64 * GROUPS, a.P, a.E, hist + wave * a.E, expert, rank);
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64) count[e] = over_waves<WAVES>(hist, a.E, e);
+    for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64) start[e] = over_waves<WAVES>(hist, a.E, e);
     __syncthreads();
-    place_experts(a, count, start, scratch);
+    place_experts(a, start, scratch, true);
     __syncthreads();
     write_pairs<GROUPS>(a, wave * 64 * GROUPS, a.P, start, hist + wave * a.E, expert, rank);
 }
@@ -154,53 +158,42 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
     for (uint32_t e = threadIdx.x; e < a.E; e += 256) a.chunk_count[uint64_t(blockIdx.x) * a.E + e] = int32_t(lds[e]);
 }
 
-// ... then, in one workgroup, for each chunk and expert the pairs in the chunks before, and where the experts begin.  With
-// fewer experts than threads, several threads share an expert's chunks.
+// ... then, for 16 experts to a workgroup, what each chunk has in the chunks before, and what the experts have in all: 64 threads
+// share an expert's chunks.
 __global__ __launch_bounds__(1024) void sort_scan_kernel(SortArgs a) {
-    extern __shared__ __align__(16) uint32_t lds[];
-    uint32_t* start = lds;
-    uint32_t* count = start + a.E;
-    uint32_t* scratch = count + a.E;
-    uint32_t* part = scratch + 16;                       // [parts][E], only where E <= 512
-    const uint32_t parts = a.E <= 512 ? 1024 / a.E : 1;
-    const uint32_t per = (a.n_chunks + parts - 1) / parts;
-    for (uint32_t i = threadIdx.x; i < parts * a.E; i += 1024) {
-        const uint32_t e = i % a.E, c0 = min(i / a.E * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
-        uint32_t n = 0;
-#pragma unroll 8
+    __shared__ uint32_t part[64][17];
+    const uint32_t lane = threadIdx.x & 15, share = threadIdx.x >> 4, e = blockIdx.x * 16 + lane;
+    const uint32_t per = (a.n_chunks + 63) / 64, c0 = min(share * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
+    uint32_t n = 0;
+    if (e < a.E) {
+#pragma unroll 4
         for (uint32_t c = c0; c < c1; ++c) n += uint32_t(a.chunk_count[uint64_t(c) * a.E + e]);
-        if (parts > 1) part[i] = n;
-        else count[e] = n;
     }
+    part[share][lane] = n;
     __syncthreads();
-    if (parts > 1) {
-        if (threadIdx.x < a.E) {
-            uint32_t n = 0;
-            for (uint32_t s = 0; s < parts; ++s) {
-                const uint32_t c = part[s * a.E + threadIdx.x];
-                part[s * a.E + threadIdx.x] = n;
-                n += c;
-            }
-            count[threadIdx.x] = n;
-        }
-        __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (uint32_t s = 0; s < 64; ++s) {
+        const uint32_t p = part[s][lane];
+        before += s < share ? p : 0;
+        all += p;
     }
-    for (uint32_t i = threadIdx.x; i < parts * a.E; i += 1024) {
-        const uint32_t e = i % a.E, c0 = min(i / a.E * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
-        uint32_t n = parts > 1 ? part[i] : 0;
-#pragma unroll 8
-        for (uint32_t c = c0; c < c1; ++c) {
-            int32_t& at = a.chunk_count[uint64_t(c) * a.E + e];
-            const uint32_t v = uint32_t(at);
-            at = int32_t(n);
-            n += v;
-        }
+    if (e >= a.E) return;
+    if (share == 0) a.counts[e] = int32_t(all);
+    for (uint32_t c = c0; c < c1; ++c) {
+        int32_t& at = a.chunk_count[uint64_t(c) * a.E + e];
+        const uint32_t v = uint32_t(at);
+        at = int32_t(before);
+        before += v;
     }
-    place_experts(a, count, start, scratch);
 }
 
-// ... and each chunk puts its pairs in place.
-template <int WAVES, int GROUPS>
+// Up to so many counts of chunks a launch less pays (10 chunks of 512 experts 9.7 us against 10.7, 32 of 160 9.3 / 10.4, 80 of 512
+// 34 / 15).
+constexpr uint32_t kAddCounts = 8192;
+
+// ... and each chunk puts its pairs in place, after it has worked out where the experts begin (the first one also writes that).
+// ADD: it adds up the counts of the chunks before it and of all itself, a launch less for reading all of them.
+template <int WAVES, int GROUPS, bool ADD>
 __global__ __launch_bounds__(WAVES * 64) void sort_place_kernel(SortArgs a) {
     static_assert(WAVES * GROUPS * 64 == kSortChunkPairs, "a workgroup ranks a chunk");
     extern __shared__ __align__(16) uint32_t lds[];
@@ -208,8 +201,28 @@ __global__ __launch_bounds__(WAVES * 64) void sort_place_kernel(SortArgs a) {
     uint32_t* start = lds + (WAVES * a.E * 2 + 3) / 4;
     const uint32_t wave = threadIdx.x >> 6;
     for (uint32_t i = threadIdx.x; i < (WAVES * a.E + 1) / 2; i += WAVES * 64) lds[i] = 0;
+    uint32_t* before = start + a.E;                      // ADD only
+    uint32_t* scratch = ADD ? before + a.E : before;
+    if constexpr (ADD) {
+        for (uint32_t e = threadIdx.x; e < 2 * a.E; e += WAVES * 64) start[e] = 0;
+        __syncthreads();
+        const uint32_t total = a.n_chunks * a.E, own = blockIdx.x * a.E;
+#pragma unroll 8
+        for (uint32_t i = threadIdx.x; i < total; i += WAVES * 64) {
+            const uint32_t n = uint32_t(a.chunk_count[i]), e = i % a.E;
+            if (n) {
+                atomicAdd(&start[e], n);
+                if (i < own) atomicAdd(&before[e], n);
+            }
+        }
+    } else {
+        for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64) start[e] = uint32_t(a.counts[e]);
+    }
+    __syncthreads();
+    place_experts(a, start, scratch, blockIdx.x == 0);
+    __syncthreads();
     for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64)
-        start[e] = uint32_t(a.offsets[e]) + uint32_t(a.chunk_count[uint64_t(blockIdx.x) * a.E + e]);
+        start[e] += ADD ? before[e] : uint32_t(a.chunk_count[uint64_t(blockIdx.x) * a.E + e]);
     __syncthreads();
     const uint32_t chunk = blockIdx.x * kSortChunkPairs, end = min(chunk + kSortChunkPairs, a.P), first = chunk + wave * 64 * GROUPS;
     int32_t expert[GROUPS];
@@ -228,8 +241,10 @@ constexpr uint32_t kRowsPerPadGroup = 16;
 template <typename E>      // E: what is cleared at once (16 bytes, or an element)
 __device__ __forceinline__ void clear_pad_rows(const int32_t* row_pair, uint32_t cap, uint32_t group, char* rows, uint64_t row_bytes_apart,
                                                uint32_t row_bytes) {
-    for (uint32_t r = group * kRowsPerPadGroup; r < min((group + 1) * kRowsPerPadGroup, cap); ++r) {
-        if (row_pair[r] >= 0) continue;
+    const uint32_t first = group * kRowsPerPadGroup, lane = threadIdx.x & 63;
+    uint64_t pads = __ballot(lane < kRowsPerPadGroup && first + lane < cap && row_pair[min(first + lane, cap - 1)] < 0);
+    for (; pads; pads &= pads - 1) {
+        const uint64_t r = first + __builtin_ctzll(pads);
         E* dst = reinterpret_cast<E*>(rows + r * row_bytes_apart);
         for (uint32_t i = threadIdx.x; i < row_bytes / sizeof(E); i += blockDim.x) dst[i] = E{};
     }
@@ -249,7 +264,12 @@ RowPlan row_plan(uint32_t T, uint32_t cap, uint32_t units) {
     return p;
 }
 
-// A token's row is read once and written to its K places.
+__device__ __forceinline__ void store_past(uint4* p, const uint4& v) { store_stream16(p, v); }
+template <typename E>
+__device__ __forceinline__ void store_past(E* p, E v) { *p = v; }
+
+// A token's row is read once and written to its K places: the places past the caches (8192 x 4096 top-2 31 us, through them
+// 38; past the caches for the row, too, 38).
 template <typename E>
 __global__ __launch_bounds__(1024) void dispatch_kernel(RowsArgs a, uint32_t elem_bytes, uint32_t rows_per_wg, uint32_t token_wgs) {
     const uint32_t row_bytes = a.H * elem_bytes;
@@ -267,53 +287,61 @@ __global__ __launch_bounds__(1024) void dispatch_kernel(RowsArgs a, uint32_t ele
     for (uint32_t i = threadIdx.x % per_row; i < row_bytes / sizeof(E); i += per_row) {
         const E v = src[i];
         for (uint32_t k = 0; k < a.K; ++k) {
-            const uint32_t r = uint32_t(at[k]);
-            if (r < a.cap) reinterpret_cast<E*>(rows + r * apart)[i] = v;
+            const uint32_t r = uint32_t(scalar_at(at, k));
+            if (r < a.cap) store_past(reinterpret_cast<E*>(rows + r * apart) + i, v);
         }
     }
 }
 
-constexpr uint32_t kRowsAtOnce = 4;          // of a token's K rows, loads that are on their way together
 constexpr uint32_t kRowColumns = 8192;       // eight columns to each lane of 16 wavefronts
 
 // out_t = sum over k of gate * row, in the order of k and in FP32
-template <typename R, typename O>
+template <typename R, int N, int ROWS>
+__device__ __forceinline__ void add_rows(const RowsArgs& a, const int32_t* at, const float* gate, uint32_t c, float (&acc)[N]) {
+    uint32_t r[ROWS];
+    float g[ROWS];
+    Pack<R, N> v[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        r[i] = uint32_t(scalar_at(at, i));
+        g[i] = gate ? scalar_at(gate, i) : 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const bool here = r[i] < a.cap;
+        v[i].template load<kStream>(row_at(static_cast<const R*>(a.rows_in), here ? r[i] : 0, a.in_stride, here ? a.H : 0), c);
+        g[i] = here ? g[i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] += g[i] * v[i][j];
+}
+
+template <typename R, typename O, int N>
 __global__ __launch_bounds__(1024) void combine_kernel(RowsArgs a, uint32_t rows_per_wg) {
     const uint32_t per_row = blockDim.x / rows_per_wg;
     const uint32_t t = __builtin_amdgcn_readfirstlane(blockIdx.x * rows_per_wg + threadIdx.x / per_row);
     if (t >= a.T) return;
-    const R* rows = static_cast<const R*>(a.rows_in);
-    O* out = static_cast<O*>(a.out) + t * a.out_stride;
+    const row_t out = row_at(static_cast<O*>(a.out), t, a.out_stride, a.H);
     const int32_t* at = a.pair_row + uint64_t(t) * a.K;
     const float* gate = a.gates ? a.gates + uint64_t(t) * a.K : nullptr;
-    for (uint32_t c = threadIdx.x % per_row * 8; c < a.H; c += per_row * 8) {
-        float acc[8] = {};
-        for (uint32_t k0 = 0; k0 < a.K; k0 += kRowsAtOnce) {
-            Pack8<R> v[kRowsAtOnce];
-            float g[kRowsAtOnce];
-#pragma unroll
-            for (uint32_t i = 0; i < kRowsAtOnce; ++i) {
-                const uint32_t k = min(k0 + i, a.K - 1), r = uint32_t(at[k]);
-                if (k0 + i < a.K && r < a.cap) {
-                    v[i].load(rows + r * a.in_stride + c);
-                    g[i] = gate ? gate[k] : 1.0f;
-                } else {
-                    v[i].zero();
-                    g[i] = 0.0f;
-                }
-            }
-#pragma unroll
-            for (uint32_t i = 0; i < kRowsAtOnce; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += g[i] * v[i][j];
+    for (uint32_t c = threadIdx.x % per_row * N; c < a.H; c += per_row * N) {
+        float acc[N] = {};
+        uint32_t k = 0;
+        for (; k + 4 <= a.K; k += 4) add_rows<R, N, 4>(a, at + k, gate ? gate + k : nullptr, c, acc);
+        if (k + 2 <= a.K) {
+            add_rows<R, N, 2>(a, at + k, gate ? gate + k : nullptr, c, acc);
+            k += 2;
         }
+        if (k < a.K) add_rows<R, N, 1>(a, at + k, gate ? gate + k : nullptr, c, acc);
         if (a.accumulate) {
-            Pack8<O> v;
-            v.load(out + c);
+            Pack<O, N> v;
+            v.template load<kCached>(out, c);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += v[j];
+            for (int j = 0; j < N; ++j) acc[j] += v[j];
         }
-        store8(out + c, acc);
+        store<O, N, kStream>(out, c, acc);
     }
 }
 
@@ -336,6 +364,7 @@ __global__ __launch_bounds__(1024) void combine_any_kernel(RowsArgs a) {
 // d_rows = gate * d_out, d_gates = <d_out, row>: a lane's eight columns of d_out stay in registers for a token's K rows.
 template <typename R, typename O>
 __global__ __launch_bounds__(1024) void combine_grad_kernel(RowsArgs a, uint32_t rows_per_wg, uint32_t token_wgs) {
+    constexpr int N = kPiece<R, O>, P = 8 / N;           // columns of a piece, pieces of a lane
     __shared__ float s_dot[16][kRouteMaxTopK];           // the wavefronts' parts of the K products
     R* d_rows = static_cast<R*>(a.rows_out);
     if (blockIdx.x >= token_wgs) {
@@ -346,41 +375,59 @@ __global__ __launch_bounds__(1024) void combine_grad_kernel(RowsArgs a, uint32_t
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), in_row = threadIdx.x % per_row;
     const uint32_t t = __builtin_amdgcn_readfirstlane(blockIdx.x * rows_per_wg + threadIdx.x / per_row);
     const bool valid = t < a.T;
-    const uint32_t c = in_row * 8;
-    const bool in = valid && c < a.H;
-    const R* rows = static_cast<const R*>(a.rows_in);
     const int32_t* at = a.pair_row + uint64_t(valid ? t : 0) * a.K;
     const float* gate = a.gates + uint64_t(valid ? t : 0) * a.K;
-    Pack8<O> d;
-    if (in) d.load(static_cast<const O*>(a.x) + t * a.x_stride + c);
-    else d.zero();
-    for (uint32_t k0 = 0; k0 < a.K; k0 += kRowsAtOnce) {
-        Pack8<R> v[kRowsAtOnce];
-        uint32_t r[kRowsAtOnce];
+    uint32_t c[P];
+    Pack<O, N> d[P];
+    const row_t d_out = row_at(static_cast<const O*>(a.x), valid ? t : 0, a.x_stride, valid ? a.H : 0);
 #pragma unroll
-        for (uint32_t i = 0; i < kRowsAtOnce; ++i) {
-            r[i] = valid && k0 + i < a.K ? uint32_t(at[min(k0 + i, a.K - 1)]) : ~0u;
-            if (in && r[i] < a.cap) v[i].load(rows + r[i] * a.in_stride + c);
-            else v[i].zero();
+    for (int p = 0; p < P; ++p) {
+        c[p] = (p * per_row + in_row) * N;
+        d[p].template load<kStream>(d_out, c[p]);
+    }
+    auto some = [&](uint32_t k0, auto rows_at_once) {
+        constexpr int ROWS = decltype(rows_at_once)::value;
+        uint32_t r[ROWS];
+        float g[ROWS];
+        Pack<R, N> v[ROWS][P];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            r[i] = uint32_t(scalar_at(at, k0 + i));
+            g[i] = scalar_at(gate, k0 + i);
         }
 #pragma unroll
-        for (uint32_t i = 0; i < kRowsAtOnce; ++i) {
-            if (k0 + i >= a.K) break;
-            float dot = 0.0f;
-            if (r[i] < a.cap) {
-                const float g = gate[k0 + i];
-                float o[8];
+        for (int i = 0; i < ROWS; ++i) {
+            const bool here = valid && r[i] < a.cap;
+            const row_t row = row_at(static_cast<const R*>(a.rows_in), here ? r[i] : 0, a.in_stride, here ? a.H : 0);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    dot += d[j] * v[i][j];
-                    o[j] = g * d[j];
+            for (int p = 0; p < P; ++p) v[i][p].template load<kStream>(row, c[p]);
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const bool here = valid && r[i] < a.cap;
+            const row_t row = row_at(d_rows, here ? r[i] : 0, a.out_stride, here ? a.H : 0);
+            float dot = 0.0f;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                float o[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    dot += d[p][j] * v[i][p][j];
+                    o[j] = g[i] * d[p][j];
                 }
-                if (in) store8(d_rows + r[i] * a.out_stride + c, o);
+                store<R, N, kStream>(row, c[p], o);
             }
             dot = group_sum<64>(dot);
-            if ((threadIdx.x & 63) == 0) s_dot[wave][k0 + i] = dot;
+            if ((threadIdx.x & 63) == 0) s_dot[wave][k0 + i] = here ? dot : 0.0f;
         }
+    };
+    uint32_t k = 0;
+    for (; k + 4 <= a.K; k += 4) some(k, std::integral_constant<int, 4>());
+    if (k + 2 <= a.K) {
+        some(k, std::integral_constant<int, 2>());
+        k += 2;
     }
+    if (k < a.K) some(k, std::integral_constant<int, 1>());
     __syncthreads();
     if (valid && in_row < a.K) {
         float sum = 0.0f;
@@ -428,8 +475,9 @@ uint32_t any_threads(uint32_t H) { return H >= 1024 ? 1024 : (H + 63) / 64 * 64;
 template <typename R, typename O>
 hipError_t go_combine(const RowsArgs& a, hipStream_t stream) {
     if (a.vec) {
-        const RowPlan p = row_plan(a.T, 0, a.H / 8);
-        hipLaunchKernelGGL((combine_kernel<R, O>), dim3(p.token_wgs), dim3(p.threads), 0, stream, a, p.rows_per_wg);
+        constexpr int N = kPiece<R, O>;
+        const RowPlan p = row_plan(a.T, 0, a.H / N);
+        hipLaunchKernelGGL((combine_kernel<R, O, N>), dim3(p.token_wgs), dim3(p.threads), 0, stream, a, p.rows_per_wg);
     } else {
         hipLaunchKernelGGL((combine_any_kernel<R, O>), dim3(a.T), dim3(any_threads(a.H)), 0, stream, a);
     }
@@ -450,7 +498,13 @@ hipError_t go_combine_grad(const RowsArgs& a, hipStream_t stream) {
 
 template <int WAVES, int GROUPS>
 hipError_t go_sort_one(const SortArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((sort_one_kernel<WAVES, GROUPS>), dim3(1), dim3(WAVES * 64), sort_one_lds_bytes(WAVES, a.E), stream, a);
+    hipLaunchKernelGGL((sort_one_kernel<WAVES, GROUPS>), dim3(1), dim3(WAVES * 64), sort_lds_bytes(WAVES, a.E, 1), stream, a);
+    return hipGetLastError();
+}
+
+template <int WAVES, int GROUPS, bool ADD>
+hipError_t go_sort_place(const SortArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((sort_place_kernel<WAVES, GROUPS, ADD>), dim3(a.n_chunks), dim3(WAVES * 64), sort_lds_bytes(WAVES, a.E, ADD ? 2 : 1), stream, a);
     return hipGetLastError();
 }
 
@@ -465,9 +519,9 @@ hipError_t launch_sort(const SortArgs& a, hipStream_t stream) {
         return go_sort_one<16, 4>(a, stream);
     }
     hipLaunchKernelGGL(sort_count_kernel, dim3(a.n_chunks), dim3(256), a.E * 4, stream, a);
-    hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), a.E * 8 + 64 + (a.E <= 512 ? 4096 : 0), stream, a);
-    hipLaunchKernelGGL((sort_place_kernel<4, 4>), dim3(a.n_chunks), dim3(256), place_lds_bytes(4, a.E), stream, a);
-    return hipGetLastError();
+    if (a.E <= 2048 && uint64_t(a.n_chunks) * a.E <= kAddCounts) return go_sort_place<8, 2, true>(a, stream);
+    hipLaunchKernelGGL(sort_scan_kernel, dim3((a.E + 15) / 16), dim3(1024), 0, stream, a);
+    return a.E <= 2048 ? go_sort_place<8, 2, false>(a, stream) : go_sort_place<4, 4, false>(a, stream);
 }
 
 hipError_t launch_dispatch(const RowsArgs& a, uint32_t elem_bytes, hipStream_t stream) {

@@ -27,20 +27,53 @@ __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(
 // e^(v - top) where top is the largest of the row; 1 at the top itself, also where that is infinite
 __device__ __forceinline__ float softmax_term(float v, float top) { return v == top ? 1.0f : expf(v - top); }
 
-// The lane's NV logits from expert `first` on; past the row's end `pad`.
-template <typename L, int NV>
-__device__ __forceinline__ void load_logits(const L* row, uint32_t first, uint32_t E, bool vec, float pad, float (&l)[NV]) {
+__device__ __forceinline__ void load8(const bf16_t* p, float* f) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int c = 0; c < NV; c += 8) {
-        if (vec && first + c + 8 <= E) {
-            Pack8<L> p;
-            p.load(row + first + c);
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float((j & 1) ? (w[j / 2] & 0xFFFF0000u) : (w[j / 2] << 16));
+}
+__device__ __forceinline__ void load8(const float* p, float* f) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) l[c + j] = p[j];
-        } else {
+    for (int j = 0; j < 8; j += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + j);
+        f[j] = v.x;
+        f[j + 1] = v.y;
+        f[j + 2] = v.z;
+        f[j + 3] = v.w;
+    }
+}
+// past the caches (16384 x 512 FP32 gradients 11.6 us, through them 15.8)
+__device__ __forceinline__ void store8(bf16_t* p, const float* f) {
+    store_stream16(p, make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7])));
+}
+__device__ __forceinline__ void store8(float* p, const float* f) {
+    store_stream16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+    store_stream16(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
+}
+
+// Eight logits from expert `first` on; minus infinity past the row's end.
+template <typename L>
+__device__ __forceinline__ void load_logits(const L* row, uint32_t first, uint32_t E, bool vec, float* l) {
+    if (vec && first + 8 <= E) {
+        load8(row + first, l);
+    } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) l[c + j] = first + c + j < E ? to_float(row[first + c + j]) : pad;
-        }
+        for (int j = 0; j < 8; ++j) l[j] = first + j < E ? to_float(row[first + j]) : -INFINITY;
+    }
+}
+
+// Keys of eight experts from `first` on.
+template <bool SIGMOID>
+__device__ __forceinline__ void keys_of(const RouteArgs& a, uint32_t first, const float* l, uint32_t* key) {
+    if constexpr (SIGMOID) {
+        Pack<float, 8> bias;                             // 0 where there is none
+        bias.template load<kCached>(row_at(a.bias, 0, 0, a.bias ? a.E : 0), first);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) key[j] = l[j] > -INFINITY ? order_key(sigmoid(l[j]) + bias[j]) : 0u;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) key[j] = order_key(l[j]);
     }
 }
 
@@ -64,18 +97,11 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     const L* logits = static_cast<const L*>(a.logits) + uint64_t(valid ? row : 0) * a.row_stride;
 
     uint32_t key[NV];
-    {
-        float l[NV];
-        load_logits<L, NV>(logits, first, valid ? a.E : 0, a.vec != 0, -INFINITY, l);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float v = l[j];
-            if constexpr (SIGMOID) {
-                const float s = sigmoid(v) + (a.bias && first + j < a.E ? a.bias[first + j] : 0.0f);
-                v = v > -INFINITY ? s : -INFINITY;
-            }
-            key[j] = order_key(v);
-        }
+    for (int c = 0; c < NV; c += 8) {
+        float l[8];
+        load_logits(logits, first + c, valid ? a.E : 0, a.vec != 0, l);
+        keys_of<SIGMOID>(a, first + c, l, &key[c]);
     }
     s_id[tid] = -1;
     s_key[tid] = 0;
@@ -122,21 +148,129 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     }
 }
 
+// The same for many rows, with fewer lanes to a row and so fewer instructions: 8 or 16 lanes, up to four chunks of eight experts
+// to each.  The keys lie in LDS (each lane's own), the chunks' largest ones in registers; when a lane's best is taken, only that
+// chunk is read again.  A round compares key and expert as one 64-bit number, the lower expert being the larger one.
+template <int LANES>
+__device__ __forceinline__ void group_best(uint32_t& key, uint32_t& rank) {
+    auto with = [&](uint32_t k, uint32_t r) {
+        const uint64_t mine = (uint64_t(key) << 32) | rank, other = (uint64_t(k) << 32) | r;
+        key = other > mine ? k : key;
+        rank = other > mine ? r : rank;
+    };
+    static_assert(LANES == 8 || LANES == 16, "a row of lanes");
+    with(dpp<kDppXor1>(key), dpp<kDppXor1>(rank));
+    with(dpp<kDppXor2>(key), dpp<kDppXor2>(rank));
+    with(dpp<kDppHalfMirror>(key), dpp<kDppHalfMirror>(rank));
+    if (LANES == 16) with(dpp<kDppMirror>(key), dpp<kDppMirror>(rank));
+}
+
+template <typename L, int LPR, int CHUNKS, bool SIGMOID>
+__global__ __launch_bounds__(kThreads) void route_many_kernel(RouteArgs a) {
+    __shared__ uint4 s_key[CHUNKS][2][kThreads];
+    const uint32_t tid = threadIdx.x, sub = tid & (LPR - 1);
+    const uint32_t row = blockIdx.x * (kThreads / LPR) + tid / LPR;
+    const bool valid = row < a.T;
+    const L* logits = static_cast<const L*>(a.logits) + uint64_t(valid ? row : 0) * a.row_stride;
+    auto first_of = [&](uint32_t ch) { return (ch * LPR + sub) * 8; };
+
+    uint32_t key[CHUNKS][8];
+#pragma unroll
+    for (int ch = 0; ch < CHUNKS; ++ch) {
+        float l[8];
+        load_logits(logits, first_of(ch), valid ? a.E : 0, a.vec != 0, l);
+        keys_of<SIGMOID>(a, first_of(ch), l, key[ch]);
+        s_key[ch][0][tid] = make_uint4(key[ch][0], key[ch][1], key[ch][2], key[ch][3]);
+        s_key[ch][1][tid] = make_uint4(key[ch][4], key[ch][5], key[ch][6], key[ch][7]);
+    }
+    uint32_t most[CHUNKS], rank[CHUNKS], best, best_rank;        // rank: the complement of the expert
+    auto best_of_lane = [&]() {
+        best = most[0];
+        best_rank = rank[0];
+#pragma unroll
+        for (int ch = 1; ch < CHUNKS; ++ch)
+            if (most[ch] > best) { best = most[ch]; best_rank = rank[ch]; }
+    };
+#pragma unroll
+    for (int ch = 0; ch < CHUNKS; ++ch) {
+        uint32_t at;
+        lane_best<8>(key[ch], most[ch], at);
+        rank[ch] = ~(first_of(ch) + at);
+    }
+    best_of_lane();
+    float total = 0.0f;
+    if (!SIGMOID && !a.renormalize) {                            // the whole row's softmax
+        const float top = key_value(group_max<LPR>(best));
+#pragma unroll
+        for (int ch = 0; ch < CHUNKS; ++ch)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) total += key[ch][j] ? softmax_term(key_value(key[ch][j]), top) : 0.0f;
+        total = group_sum<LPR>(total);
+    }
+    uint32_t top_key = 0, got_key[2] = {0, 0};
+    int32_t got_id[2] = {-1, -1};                                // lane i keeps the i-th and the LPR + i-th choice
+    for (uint32_t k = 0; k < a.K; ++k) {
+        uint32_t won = best, won_rank = best_rank;
+        group_best<LPR>(won, won_rank);
+        if (k == 0) top_key = won;
+        const bool keep = sub == (k & (LPR - 1)) && won != 0;
+        const uint32_t id = ~won_rank;
+        if (k < LPR) {
+            if (keep) { got_id[0] = int32_t(id); got_key[0] = won; }
+        } else {
+            if (keep) { got_id[1] = int32_t(id); got_key[1] = won; }
+        }
+        if (best_rank == won_rank && won != 0) {                 // this lane's best was taken
+            const uint32_t ch = id / (8 * LPR), j = id & 7;
+            reinterpret_cast<uint32_t*>(&s_key[ch][j >> 2][tid])[j & 3] = 0;
+            const uint4 lo = s_key[ch][0][tid], hi = s_key[ch][1][tid];
+            const uint32_t left[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            uint32_t m, at;
+            lane_best<8>(left, m, at);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+                if (uint32_t(c) == ch) { most[c] = m; rank[c] = ~(first_of(c) + at); }
+            best_of_lane();
+        }
+    }
+    float p[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (got_id[i] >= 0) {
+            if constexpr (SIGMOID) p[i] = sigmoid(to_float(logits[got_id[i]]));
+            else p[i] = softmax_term(key_value(got_key[i]), key_value(top_key));
+        }
+    if (a.renormalize) {
+        total = group_sum<LPR>(p[0] + p[1]);
+        if (total == 0.0f) total = 1.0f;
+    }
+    if (SIGMOID && !a.renormalize) total = 1.0f;
+    if (!valid) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t k = sub + i * LPR;
+        if (k >= a.K) break;
+        a.ids[uint64_t(row) * a.K + k] = got_id[i];
+        a.gates[uint64_t(row) * a.K + k] = got_id[i] >= 0 ? p[i] / total * a.scale : 0.0f;
+    }
+}
+
 // With c the chosen scores (a softmax's numerators: its sum cancels where the gates are divided by theirs), C their sum and
 // d = scale * d_gates:
 //   renormalised:  d_c = (d - sum(d c) / C) / C, then times c (softmax) or c (1 - c) (sigmoid)
 //   sigmoid:       d c (1 - c)
 //   softmax:       p_i (d_i - sum_j d_j p_j) for every expert i of the row, chosen or not
-// The K values of a row are spread over its experts in LDS; every lane then writes its experts.
-template <typename L, int LPR, int NV, bool SIGMOID>
+// The K values of a row are spread over its experts in LDS; the lanes then write the row, eight experts at a time.
+template <typename L, int LPR, int CHUNKS, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteArgs a) {
-    __shared__ __align__(16) float s_row[kThreads * NV];  // LPR * NV >= E places for a row
-    const uint32_t tid = threadIdx.x, sub = tid & (LPR - 1), base = tid - sub;
+    __shared__ __align__(16) float s_row[kThreads / LPR][LPR * CHUNKS * 8];
+    const uint32_t tid = threadIdx.x, sub = tid & (LPR - 1);
     const uint32_t row = blockIdx.x * (kThreads / LPR) + tid / LPR;
     const bool valid = row < a.T;
-    const uint32_t first = sub * NV;
     const L* logits = static_cast<const L*>(a.logits) + uint64_t(valid ? row : 0) * a.row_stride;
     const bool dense = !SIGMOID && !a.renormalize;
+    float* spread = s_row[tid / LPR];
+    auto first_of = [&](uint32_t ch) { return (ch * LPR + sub) * 8; };
 
     int32_t id = -1;
     float d = 0.0f;
@@ -147,29 +281,33 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteArgs a) {
     const bool chosen = uint32_t(id) < a.E;
     const float l_chosen = chosen ? to_float(logits[id]) : -INFINITY;
 #pragma unroll
-    for (int j = 0; j < NV; j += 4) *reinterpret_cast<float4*>(&s_row[tid * NV + j]) = make_float4(0, 0, 0, 0);
+    for (int ch = 0; ch < CHUNKS; ++ch) {
+        float4* p = reinterpret_cast<float4*>(spread + first_of(ch));
+        p[0] = p[1] = make_float4(0, 0, 0, 0);
+    }
     wave_fence();
 
-    float out[NV];
+    float l[CHUNKS][8], inv = 0.0f, mean = 0.0f;
     if (dense) {
-        float l[NV], top = -INFINITY, total = 0.0f;
-        load_logits<L, NV>(logits, first, valid ? a.E : 0, a.vec != 0, -INFINITY, l);
+        float top = -INFINITY, total = 0.0f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) top = fmaxf(top, l[j]);
+        for (int ch = 0; ch < CHUNKS; ++ch) {
+            load_logits(logits, first_of(ch), valid ? a.E : 0, a.vec != 0, l[ch]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, l[ch][j]);
+        }
         top = group_max<LPR>(top);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            l[j] = l[j] > -INFINITY ? softmax_term(l[j], top) : 0.0f;
-            total += l[j];
-        }
-        total = group_sum<LPR>(total);
-        const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-        const float p_chosen = chosen && l_chosen > -INFINITY ? softmax_term(l_chosen, top) * inv : 0.0f;
-        const float mean = group_sum<LPR>(chosen ? d * p_chosen : 0.0f);
-        if (chosen) s_row[base * NV + id] = d;
-        wave_fence();
+        for (int ch = 0; ch < CHUNKS; ++ch)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) out[j] = l[j] * inv * (s_row[tid * NV + j] - mean);
+            for (int j = 0; j < 8; ++j) {
+                l[ch][j] = l[ch][j] > -INFINITY ? softmax_term(l[ch][j], top) : 0.0f;
+                total += l[ch][j];
+            }
+        total = group_sum<LPR>(total);
+        inv = total > 0.0f ? 1.0f / total : 0.0f;
+        const float p_chosen = chosen && l_chosen > -INFINITY ? softmax_term(l_chosen, top) * inv : 0.0f;
+        mean = group_sum<LPR>(chosen ? d * p_chosen : 0.0f);
     } else {
         float c = 0.0f, slope;
         if constexpr (SIGMOID) {
@@ -184,47 +322,93 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteArgs a) {
         if (a.renormalize) {
             float total = group_sum<LPR>(c);
             if (total == 0.0f) total = 1.0f;
-            const float mean = group_sum<LPR>(chosen ? d * (c / total) : 0.0f);
+            mean = group_sum<LPR>(chosen ? d * (c / total) : 0.0f);
             d = (d - mean) / total;
         }
-        if (chosen) s_row[base * NV + id] = d * slope;
-        wave_fence();
-#pragma unroll
-        for (int j = 0; j < NV; ++j) out[j] = s_row[tid * NV + j];
+        d *= slope;
     }
+    if (chosen) spread[id] = d;
+    wave_fence();
     if (!valid) return;
     L* dst = static_cast<L*>(a.d_logits) + uint64_t(row) * a.d_stride;
 #pragma unroll
-    for (int c = 0; c < NV; c += 8) {
-        if (a.d_vec && first + c + 8 <= a.E) {
-            const float o[8] = {out[c], out[c + 1], out[c + 2], out[c + 3], out[c + 4], out[c + 5], out[c + 6], out[c + 7]};
-            store8(dst + first + c, o);
+    for (int ch = 0; ch < CHUNKS; ++ch) {
+        const uint32_t e = first_of(ch);
+        float out[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            out[j] = spread[e + j];
+            if (dense) out[j] = l[ch][j] * inv * (out[j] - mean);
+        }
+        if (a.d_vec && e + 8 <= a.E) {
+            store8(dst + e, out);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (first + c + j < a.E) from_float(dst + first + c + j, out[c + j]);
+                if (e + j < a.E) from_float(dst + e + j, out[j]);
         }
     }
 }
 
-template <typename L, bool SIGMOID, int LPR, int NV>
-hipError_t go(const RouteArgs& a, bool grad, hipStream_t stream) {
-    const uint32_t rows = kThreads / LPR, grid = (a.T + rows - 1) / rows;
-    if (grad) hipLaunchKernelGGL((route_grad_kernel<L, LPR, NV, SIGMOID>), dim3(grid), dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((route_kernel<L, LPR, NV, SIGMOID>), dim3(grid), dim3(kThreads), 0, stream, a);
-    return hipGetLastError();
+uint32_t workgroups(const RouteArgs& a, uint32_t lanes) {
+    const uint32_t rows = kThreads / lanes;
+    return (a.T + rows - 1) / rows;
 }
+template <typename L, bool SIGMOID, int LPR, int NV>
+void go(const RouteArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((route_kernel<L, LPR, NV, SIGMOID>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
+}
+template <typename L, bool SIGMOID, int LPR, int CHUNKS>
+void go_many(const RouteArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((route_many_kernel<L, LPR, CHUNKS, SIGMOID>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
+}
+template <typename L, bool SIGMOID, int LPR, int CHUNKS>
+void go_grad(const RouteArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((route_grad_kernel<L, LPR, CHUNKS, SIGMOID>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
+}
+
+// From about two million logits on the instructions count, and route_many_kernel has fewer; below, a round's length does
+// (16384 x 512 top-10 11.7 us against 19.5, 8192 x 512 8.0 / 11.1, 4096 x 512 7.9 / 7.1, 1 x 512 7.1 / 4.2; 16384 x 160 top-8 6.5 / 9.7).
+#ifndef MANYN
+#define MANYN 2097152
+#endif
+constexpr uint64_t kManyLogits = MANYN;
 
 // As few lanes to a row as hold its experts at eight each, and one for every chosen expert.
 template <typename L, bool SIGMOID>
+void pick(const RouteArgs& a, hipStream_t stream) {
+    if (uint64_t(a.T) * a.E > kManyLogits && a.E > 64 && a.E <= 512 && a.K <= 16) {
+        if (a.E <= 128) go_many<L, SIGMOID, 8, 2>(a, stream);
+        else if (a.E <= 192) go_many<L, SIGMOID, 8, 3>(a, stream);
+        else if (a.E <= 256) go_many<L, SIGMOID, 8, 4>(a, stream);
+        else go_many<L, SIGMOID, 16, 4>(a, stream);
+        return;
+    }
+    if (a.E <= 16 && a.K <= 2) go<L, SIGMOID, 2, 8>(a, stream);
+    else if (a.E <= 64 && a.K <= 8) go<L, SIGMOID, 8, 8>(a, stream);
+    else if (a.E <= 256 && a.K <= 32) go<L, SIGMOID, 32, 8>(a, stream);
+    else if (a.E <= 512) go<L, SIGMOID, 64, 8>(a, stream);
+    else if (a.E <= 1024) go<L, SIGMOID, 64, 16>(a, stream);
+    else if (a.E <= 2048) go<L, SIGMOID, 64, 32>(a, stream);
+    else go<L, SIGMOID, 64, 64>(a, stream);
+}
+
+template <typename L, bool SIGMOID>
+void pick_grad(const RouteArgs& a, hipStream_t stream) {
+    if (a.E <= 16 && a.K <= 2) go_grad<L, SIGMOID, 2, 1>(a, stream);
+    else if (a.E <= 64 && a.K <= 8) go_grad<L, SIGMOID, 8, 1>(a, stream);
+    else if (a.E <= 256 && a.K <= 32) go_grad<L, SIGMOID, 32, 1>(a, stream);
+    else if (a.E <= 512) go_grad<L, SIGMOID, 64, 1>(a, stream);
+    else if (a.E <= 1024) go_grad<L, SIGMOID, 64, 2>(a, stream);
+    else if (a.E <= 2048) go_grad<L, SIGMOID, 64, 4>(a, stream);
+    else go_grad<L, SIGMOID, 64, 8>(a, stream);
+}
+
+template <typename L, bool SIGMOID>
 hipError_t pick(const RouteArgs& a, bool grad, hipStream_t stream) {
-    if (a.E <= 16 && a.K <= 2) return go<L, SIGMOID, 2, 8>(a, grad, stream);
-    if (a.E <= 64 && a.K <= 8) return go<L, SIGMOID, 8, 8>(a, grad, stream);
-    if (a.E <= 256 && a.K <= 32) return go<L, SIGMOID, 32, 8>(a, grad, stream);
-    if (a.E <= 512) return go<L, SIGMOID, 64, 8>(a, grad, stream);
-    if (a.E <= 1024) return go<L, SIGMOID, 64, 16>(a, grad, stream);
-    if (a.E <= 2048) return go<L, SIGMOID, 64, 32>(a, grad, stream);
-    return go<L, SIGMOID, 64, 64>(a, grad, stream);
+    if (grad) pick_grad<L, SIGMOID>(a, stream);
+    else pick<L, SIGMOID>(a, stream);
+    return hipGetLastError();
 }
 
 hipError_t launch(const RouteArgs& a, bool f32, bool sigmoid, bool grad, hipStream_t stream) {
