@@ -148,14 +148,24 @@ __device__ __forceinline__ T scalar_at(const T* p, uint64_t i) {
 template <typename A, typename B>
 constexpr int kPiece = sizeof(A) == 2 && sizeof(B) == 2 ? 8 : 4;
 
-// 1 / (1 + e^-v), each step rounded as written (the choice of experts goes by these bits).  The quotient by one Newton step on
-// the hardware's reciprocal (Markstein 1990): equal to the division for every significand of the divisor, which the tests go
-// through; where the result leaves the normal numbers, the division itself.
-__device__ __forceinline__ float sigmoid(float v) {
-    const float d = 1.0f + expf(-v);
-    if (d > 0x1p100f) return 1.0f / d;
-    const float r = __builtin_amdgcn_rcpf(d);
-    return fmaf(fmaf(-d, r, 1.0f), r, r);
+// 1 / (1 + e^-v), each step rounded as written (the choice of experts goes by these bits).
+__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
+
+// The same of eight values.  The quotient by one Newton step on the hardware's reciprocal (Markstein 1990): equal to the division for
+// every significand of the divisor, which the tests go through; where one leaves the normal numbers, the division itself.
+__device__ __forceinline__ void sigmoid8(const float* v, float* s) {
+    float d[8], most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        d[j] = 1.0f + expf(-v[j]);
+        most = fmaxf(most, d[j]);
+        const float r = __builtin_amdgcn_rcpf(d[j]);
+        s[j] = fmaf(fmaf(-d[j], r, 1.0f), r, r);
+    }
+    if (most > 0x1p100f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = 1.0f / d[j];
+    }
 }
 
 // Row kernels: `waves` wavefronts to a row of eight elements per lane, and so many rows that a workgroup has four wavefronts

@@ -69,8 +69,12 @@ __device__ __forceinline__ void keys_of(const RouteArgs& a, uint32_t first, cons
     if constexpr (SIGMOID) {
         Pack<float, 8> bias;                             // 0 where there is none
         bias.template load<kCached>(row_at(a.bias, 0, 0, a.bias ? a.E : 0), first);
+        float v[8], score[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) key[j] = l[j] > -INFINITY ? order_key(sigmoid(l[j]) + bias[j]) : 0u;
+        for (int j = 0; j < 8; ++j) v[j] = l[j] > -INFINITY ? l[j] : 0.0f;
+        sigmoid8(v, score);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) key[j] = l[j] > -INFINITY ? order_key(score[j] + bias[j]) : 0u;
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) key[j] = order_key(l[j]);
@@ -150,21 +154,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 
 // The same for many rows, with fewer lanes to a row and so fewer instructions: 8 or 16 lanes, up to four chunks of eight experts
 // to each.  The keys lie in LDS (each lane's own), the chunks' largest ones in registers; when a lane's best is taken, only that
-// chunk is read again.  A round compares key and expert as one 64-bit number, the lower expert being the larger one.
-template <int LANES>
-__device__ __forceinline__ void group_best(uint32_t& key, uint32_t& rank) {
-    auto with = [&](uint32_t k, uint32_t r) {
-        const uint64_t mine = (uint64_t(key) << 32) | rank, other = (uint64_t(k) << 32) | r;
-        key = other > mine ? k : key;
-        rank = other > mine ? r : rank;
-    };
-    static_assert(LANES == 8 || LANES == 16, "a row of lanes");
-    with(dpp<kDppXor1>(key), dpp<kDppXor1>(rank));
-    with(dpp<kDppXor2>(key), dpp<kDppXor2>(rank));
-    with(dpp<kDppHalfMirror>(key), dpp<kDppHalfMirror>(rank));
-    if (LANES == 16) with(dpp<kDppMirror>(key), dpp<kDppMirror>(rank));
-}
-
+// chunk is read again.  Of equal keys the largest complement of an expert's number wins.
 template <typename L, int LPR, int CHUNKS, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void route_many_kernel(RouteArgs a) {
     __shared__ uint4 s_key[CHUNKS][2][kThreads];
@@ -210,8 +200,8 @@ __global__ __launch_bounds__(kThreads) void route_many_kernel(RouteArgs a) {
     uint32_t top_key = 0, got_key[2] = {0, 0};
     int32_t got_id[2] = {-1, -1};                                // lane i keeps the i-th and the LPR + i-th choice
     for (uint32_t k = 0; k < a.K; ++k) {
-        uint32_t won = best, won_rank = best_rank;
-        group_best<LPR>(won, won_rank);
+        const uint32_t won = group_max<LPR>(best);
+        const uint32_t won_rank = group_max<LPR>(best == won ? best_rank : 0u);
         if (k == 0) top_key = won;
         const bool keep = sub == (k & (LPR - 1)) && won != 0;
         const uint32_t id = ~won_rank;
@@ -367,17 +357,15 @@ void go_grad(const RouteArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((route_grad_kernel<L, LPR, CHUNKS, SIGMOID>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
 }
 
-// From about two million logits on the instructions count, and route_many_kernel has fewer; below, a round's length does
-// (16384 x 512 top-10 11.7 us against 19.5, 8192 x 512 8.0 / 11.1, 4096 x 512 7.9 / 7.1, 1 x 512 7.1 / 4.2; 16384 x 160 top-8 6.5 / 9.7).
-#ifndef MANYN
-#define MANYN 2097152
-#endif
-constexpr uint64_t kManyLogits = MANYN;
+// With many rows the instructions count, and route_many_kernel has fewer; below, a round's length does (us, route_many_kernel /
+// route_kernel: 16384 x 512 top-10 11.0 / 19.5, 8192 x 512 7.5 / 11.1, 4096 x 512 7.5 / 7.1, 1 x 512 7.1 / 4.1; 16384 x 160 top-8 by
+// sigmoids 8.0 / 14.0, 8192 x 160 7.1 / 7.8, 4096 x 160 8.2 / 5.4).
+constexpr uint32_t kManyRows = 4096;
 
 // As few lanes to a row as hold its experts at eight each, and one for every chosen expert.
 template <typename L, bool SIGMOID>
 void pick(const RouteArgs& a, hipStream_t stream) {
-    if (uint64_t(a.T) * a.E > kManyLogits && a.E > 64 && a.E <= 512 && a.K <= 16) {
+    if (a.T > kManyRows && a.E > 64 && a.E <= 512 && a.K <= 16) {
         if (a.E <= 128) go_many<L, SIGMOID, 8, 2>(a, stream);
         else if (a.E <= 192) go_many<L, SIGMOID, 8, 3>(a, stream);
         else if (a.E <= 256) go_many<L, SIGMOID, 8, 4>(a, stream);
