@@ -460,8 +460,8 @@ int fluxmoe_balanced_split(double beta_gpu, double beta_cpu, uint32_t experts_pe
  * ascending expert.  A gate is its expert's score without the bias, with FLUXMOE_ROUTE_RENORMALIZE divided by
  * the sum over the chosen ones, times `scale`.
  * An expert whose logit (or score + bias) is minus infinity or not a number is never chosen: places that stay
- * empty get expert -1 and gate 0, a row with nothing to choose only such.  (fluxmoe_expert_ffn takes such pairs
- * with FLUXMOE_FFN_SKIP_UNMAPPED.)
+ * empty get expert -1 and gate 0, a row with nothing to choose only such.  fluxmoe_expert_ffn adds nothing for such
+ * a pair and reports it in the device error word; fluxmoe_sort_tokens drops it.
  */
 #define FLUXMOE_ROUTE_SIGMOID 1u
 #define FLUXMOE_ROUTE_RENORMALIZE 2u
@@ -517,7 +517,7 @@ int fluxmoe_combine_grad(const void* d_out, uint32_t out_type, uint64_t d_out_st
  *   w_pre and w_post weight_type [hidden]; gate device float: NULL, [T] with FLUXMOE_NORM_GATE_TOKEN or
  *   [hidden] with FLUXMOE_NORM_GATE_CHANNEL, its sigmoid with FLUXMOE_NORM_GATE_SIGMOID.
  *   FLUXMOE_NORM_ZERO_CENTRED: the weights are 1 + w.
- * residual_out may be the residual's own rows.  Strides of 0 mean `hidden`.
+ * residual_out may be the residual's own rows (then with their stride).  Strides of 0 mean `hidden`.
  */
 #define FLUXMOE_NORM_GATE_TOKEN 1u
 #define FLUXMOE_NORM_GATE_CHANNEL 2u
@@ -539,7 +539,7 @@ int fluxmoe_block_norm(const fluxmoe_norm_desc* desc, uint32_t T, const void* y,
  * elsewhere, or NULL (0); d_normed BF16.  d_residual (residual_type) and d_y (y_type) have the rows of theirs;
  * d_gate, d_w_post, d_w_pre are float, overwritten, and summed over what the gate and the weights were spread over.
  * d_y, d_gate and d_w_post are given where y, gate and w_post are.  d_residual may be d_residual_out's own rows, d_y
- * those of y.  workspace: device, 16-byte aligned, fluxmoe_block_norm_grad_workspace_bytes. */
+ * those of y (then with their strides).  workspace: device, 16-byte aligned, fluxmoe_block_norm_grad_workspace_bytes. */
 uint64_t fluxmoe_block_norm_grad_workspace_bytes(uint32_t T, uint32_t hidden);
 int fluxmoe_block_norm_grad(const fluxmoe_norm_desc* desc, uint32_t T, const void* y, const void* residual_out,
                             const float* gate, const void* w_post, const void* w_pre, const void* d_residual_out,

@@ -321,6 +321,8 @@ int fluxmoe_block_norm_grad(const fluxmoe_norm_desc* d, uint32_t T, const void* 
     if ((d_w_post != nullptr) != (w_post != nullptr) || (d_gate != nullptr) != (gate != nullptr) || (d_y != nullptr) != (y != nullptr))
         return set_error(FLUXMOE_EINVAL, "d_y, d_gate and d_w_post go with y, gate and w_post");
     if (!d_w_pre || !w_pre || (T && (!residual_out || !d_normed || !d_residual))) return set_error(FLUXMOE_EINVAL, "NULL argument");
+    if ((d_residual == d_residual_out && a.d_residual_stride != a.d_residual_out_stride) || (d_y && d_y == y && a.d_y_stride != a.y_stride))
+        return set_error(FLUXMOE_EINVAL, "a gradient in its input's place must have its stride");
     const uint32_t yb = elem_bytes(d->y_type), rb = elem_bytes(d->residual_type);
     if (!aligned(d_residual_out, rb) || !aligned(d_normed, 2) || !aligned(d_residual, rb) || !aligned(d_y, yb) || !aligned(d_gate, 4) ||
         !aligned(d_w_post, 4) || !aligned(d_w_pre, 4))

@@ -347,11 +347,34 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(NormArgs a, uint32_t wa
             if (c[0] == 0 && t < a.T) a.d_gate[t] = a.scale * dot * (a.gate_sigmoid ? g * (1.0f - g) : 1.0f);
         }
     }
-    const uint32_t part = blockIdx.x * rows_per_wg + mine;
+    // the sums of the rows side by side in a workgroup become one, by way of LDS and in their order
+    __shared__ float s_sum[2][2048];                     // [row][column]: 4 rows of up to 512, or 2 of up to 1024
+    if (rows_per_wg > 1) {
+        if (mine > 0) {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    s_sum[0][mine * per_row * 8 + c[p] + j] = sum_pre[p][j];
+                    if (FACTORS) s_sum[1][mine * per_row * 8 + c[p] + j] = sum_y[p][j];
+                }
+        }
+        __syncthreads();
+        if (mine > 0) return;
+        for (uint32_t i = 1; i < rows_per_wg; ++i)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    sum_pre[p][j] += s_sum[0][i * per_row * 8 + c[p] + j];
+                    if (FACTORS) sum_y[p][j] += s_sum[1][i * per_row * 8 + c[p] + j];
+                }
+    }
+    const row_t to_pre = row_at(partial_row(a, 0, blockIdx.x), 0, 0, a.H), to_y = row_at(partial_row(a, 1, blockIdx.x), 0, 0, a.H);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        store<float, N, kCached>(row_at(partial_row(a, 0, part), 0, 0, a.H), c[p], sum_pre[p]);
-        if (FACTORS) store<float, N, kCached>(row_at(partial_row(a, 1, part), 0, 0, a.H), c[p], sum_y[p]);
+        store<float, N, kCached>(to_pre, c[p], sum_pre[p]);
+        if (FACTORS) store<float, N, kCached>(to_y, c[p], sum_y[p]);
     }
 }
 
@@ -495,7 +518,7 @@ template <typename Y, typename R, Mode MODE>
 void go_grad_rows(NormArgs& a, hipStream_t stream) {
     const RowShape s = row_shape(a.H);
     const uint32_t wgs = walkers(s, a.T, grad_waves<Y, R>(a.H));
-    a.n_partials = wgs * s.rows_per_wg;
+    a.n_partials = wgs;
     if (a.d_residual_out) hipLaunchKernelGGL((norm_grad_kernel<Y, R, MODE, true>), dim3(wgs), dim3(s.threads()), 0, stream, a, s.waves, s.rows_per_wg);
     else hipLaunchKernelGGL((norm_grad_kernel<Y, R, MODE, false>), dim3(wgs), dim3(s.threads()), 0, stream, a, s.waves, s.rows_per_wg);
 }
@@ -525,7 +548,7 @@ hipError_t go_grad(NormArgs a, bool vec, hipStream_t stream) {
 
 uint32_t norm_grad_partials(uint32_t T, uint32_t H) {
     const RowShape s = row_shape(H);
-    const uint32_t rows = walkers(s, T, kMostGradWaves) * s.rows_per_wg, any = T < 256 ? T : 256;
+    const uint32_t rows = walkers(s, T, kMostGradWaves), any = T < 256 ? T : 256;
     return H <= kRowColumns && rows > any ? rows : any;
 }
 

@@ -29,20 +29,25 @@ __device__ __forceinline__ void rank_pairs(const int32_t* ids, uint32_t first, u
         expert[g] = e;
     }
     const uint32_t bits = 32 - __builtin_clz(E);         // minus one has the bit above those of the numbers below E set, too
+    uint64_t same[GROUPS];
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-        uint64_t same = ~0ull;
-        for (uint32_t b = 0; b < bits; ++b) {
+    for (int g = 0; g < GROUPS; ++g) same[g] = ~0ull;
+    for (uint32_t b = 0; b < bits; ++b) {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
             const bool set = (expert[g] >> b) & 1;
             const uint64_t with = __ballot(set);
-            same &= set ? with : ~with;
+            same[g] &= set ? with : ~with;
         }
-        const uint32_t below = __builtin_popcountll(same & ((1ull << lane) - 1));
+    }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        const uint32_t below = __builtin_popcountll(same[g] & ((1ull << lane) - 1));
         uint32_t had = 0;
         if (expert[g] >= 0) had = hist[expert[g]];
         wave_fence();
         rank[g] = had + below;
-        if (expert[g] >= 0 && below == 0) hist[expert[g]] = uint16_t(had + __builtin_popcountll(same));
+        if (expert[g] >= 0 && below == 0) hist[expert[g]] = uint16_t(had + __builtin_popcountll(same[g]));
         wave_fence();
     }
 }

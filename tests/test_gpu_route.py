@@ -214,6 +214,31 @@ def test_gradient_against_differences(score, renormalize):
         assert bool(((got[:, e].cpu().double() - slope).abs() <= tol).all())
 
 
+def test_sigmoid_scores_are_the_divisions():
+    """The scores' quotients come by a Newton step; every significand of 1 + e^-logit comes up for logits of -1.1 to 0.  Two
+    neighbouring logits in a row: the higher one is chosen unless the divisions make the two scores equal."""
+    step = 2.0 ** -24
+    for first in range(0, int(1.1 / step), 1 << 20):
+        low = -(torch.arange(first + 1, first + 1 + (1 << 20), device="cuda", dtype=torch.float32) * step)
+        logits = torch.stack([low, low + step], dim=1)
+        s = 1.0 / (1.0 + torch.exp(-logits))
+        ids = torch.empty(1 << 20, 1, dtype=torch.int32, device="cuda")
+        gates = torch.empty(1 << 20, 1, device="cuda")
+        M.route(logits, ids, gates, score="sigmoid", renormalize=False)
+        higher = s[:, 1] > s[:, 0]
+        assert torch.equal(ids[:, 0] == 1, higher)
+        assert torch.equal(gates[:, 0], torch.where(higher, s[:, 1], s[:, 0]))
+
+
+def test_scores_below_the_normal_numbers():
+    logits = torch.tensor([[-103.0, -87.0, -88.5, -95.0, -104.5, -200.0, -1e30, -math.inf]], device="cuda")
+    s = 1.0 / (1.0 + torch.exp(-logits))
+    ids, gates = run(logits, 8, score="sigmoid", renormalize=False)
+    want = torch.sort(torch.where(torch.isneginf(logits), -1.0, s), dim=1, descending=True, stable=True)
+    assert torch.equal(ids, torch.where(want.values.cpu() >= 0, want.indices.cpu(), -1))
+    assert torch.equal(gates, want.values.clamp(min=0).cpu())
+
+
 def test_no_tokens_and_an_expert_out_of_range():
     empty = torch.empty(0, 8, device="cuda")
     M.route(empty, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))

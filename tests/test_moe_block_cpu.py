@@ -144,6 +144,11 @@ def test_norm_grad_refuses(status, kw):
     refused(status, norm_grad, desc(), **kw)
 
 
+def test_norm_grad_refuses_another_stride_in_an_inputs_place():
+    assert "stride" in refused(-1, norm_grad, desc(d_residual_stride=128))
+    assert "stride" in refused(-1, norm_grad, desc(d_y_stride=128), dr=2 * P, do=4 * P)
+
+
 def test_tensors_are_checked_before_the_library_is_called():
     x = torch.zeros(4, 8)
     for call in (lambda: M.route(x, torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)),
