@@ -144,7 +144,9 @@ __device__ __forceinline__ T scalar_at(const T* p, uint64_t i) {
     return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[i];
 }
 
-// What a lane loads at once of rows of types A and B: eight columns where both are BF16, four where one is FP32.
+// What a lane loads at once of rows of types A and B: eight columns where both are BF16, four where one is FP32, so that a lane's
+// load has at most 16 bytes and a wavefront's no gaps between lanes (FP32 rows added up by token: pieces of four 62 us, of eight 68;
+// BF16 to FP32 34 / 35; BF16 to BF16 42 / 34).
 template <typename A, typename B>
 constexpr int kPiece = sizeof(A) == 2 && sizeof(B) == 2 ? 8 : 4;
 
