@@ -15,77 +15,90 @@ namespace {
 // expert, so that a pair's rank among its wavefront's pairs of that expert is what the wavefront had before plus the number
 // of equal lanes below.  The wavefronts' counts, added up over wavefronts (and chunks) and experts, give where each begins.
 // A few bytes for each pair: bound by the launches and by the steps that follow each other inside them.  Measured (us, a launch's own
-// 2.1 included): 10 pairs 3.1; 4096 pairs of 160 experts in one workgroup 7.5; 16384 of 8 6.5 (two launches); 81920 of 512 12.0 and
-// 655360 of 512 21 (three).
+// 2.1 included): 10 pairs 2.8; 4096 pairs of 160 experts in one workgroup 5.9; 16384 of 8 5.9 (two launches); 81920 of 512 11.2 and
+// 655360 of 512 19 (three).
 
-// Pairs of the expert before the pair, within this wavefront's 64 * GROUPS pairs.  hist: this wavefront's counts, [E], zero
-// at the start.  e < 0: no expert of the layer.
+// The experts of this wavefront's 64 * GROUPS pairs, -1: none of the layer's.
 template <int GROUPS>
-__device__ __forceinline__ void rank_pairs(const int32_t* ids, uint32_t first, uint32_t end, uint32_t E, uint16_t* hist,
-                                           int32_t (&expert)[GROUPS], uint32_t (&rank)[GROUPS]) {
-    const uint32_t lane = threadIdx.x & 63;
+__device__ __forceinline__ void load_experts(const int32_t* ids, uint32_t first, uint32_t end, uint32_t E, int32_t (&expert)[GROUPS]) {
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-        const uint32_t p = first + g * 64 + lane;
-        int32_t e = p < end ? ids[p] : -1;
-        if (uint32_t(e) >= E) e = -1;
-        expert[g] = e;
+        const uint32_t p = first + g * 64 + (threadIdx.x & 63);
+        const int32_t e = p < end ? ids[p] : -1;
+        expert[g] = uint32_t(e) < E ? e : -1;
     }
+}
+
+// Pairs of the expert before the pair, within this wavefront's.  hist: this wavefront's counts, [E], zero at the start.
+template <int GROUPS>
+__device__ __forceinline__ void rank_pairs(uint32_t E, uint16_t* hist, const int32_t (&expert)[GROUPS], uint32_t (&rank)[GROUPS]) {
     const uint32_t bits = 32 - __builtin_clz(E);         // minus one has the bit above those of the numbers below E set, too
-    uint64_t same[GROUPS];
+    uint32_t same[GROUPS][2];                            // the lanes with the lane's expert, low and high half
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) same[g] = ~0ull;
+    for (int g = 0; g < GROUPS; ++g) same[g][0] = same[g][1] = ~0u;
     for (uint32_t b = 0; b < bits; ++b) {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-            const bool set = (expert[g] >> b) & 1;
-            const uint64_t with = __ballot(set);
-            same[g] &= set ? with : ~with;
+            const uint32_t mine = uint32_t(__builtin_amdgcn_sbfe(expert[g], b, 1));       // all bits the lane's bit b
+            const uint64_t with = __ballot(mine != 0);
+            same[g][0] &= ~(uint32_t(with) ^ mine);
+            same[g][1] &= ~(uint32_t(with >> 32) ^ mine);
         }
     }
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-        const uint32_t below = __builtin_popcountll(same[g] & ((1ull << lane) - 1));
+        const uint32_t below = __builtin_amdgcn_mbcnt_hi(same[g][1], __builtin_amdgcn_mbcnt_lo(same[g][0], 0));
         uint32_t had = 0;
         if (expert[g] >= 0) had = hist[expert[g]];
         wave_fence();
         rank[g] = had + below;
-        if (expert[g] >= 0 && below == 0) hist[expert[g]] = uint16_t(had + __builtin_popcountll(same[g]));
+        if (expert[g] >= 0 && below == 0) hist[expert[g]] = uint16_t(had + __builtin_popcount(same[g][0]) + __builtin_popcount(same[g][1]));
         wave_fence();
     }
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
+    return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, ROWS, 0xF, false));
+}
+
 // Exclusive prefix sum of one value per thread over the workgroup; `scratch` holds a value per wavefront.
+template <int WAVES>
 __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* scratch, uint32_t& total) {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-    uint32_t incl = v;
-#pragma unroll
-    for (uint32_t d = 1; d < 64; d *= 2) {
-        const uint32_t o = __shfl_up(incl, d, 64);
-        if (lane >= d) incl += o;
-    }
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t incl = v;                                   // within 16 lanes, then across the four sixteens
+    incl += dpp_or_0<0x111, 0xF>(incl);                  // the lane 1, 2, 4, 8 below
+    incl += dpp_or_0<0x112, 0xF>(incl);
+    incl += dpp_or_0<0x114, 0xF>(incl);
+    incl += dpp_or_0<0x118, 0xF>(incl);
+    incl += dpp_or_0<0x142, 0xA>(incl);                  // the last lane of the sixteen before, to the second and fourth
+    incl += dpp_or_0<0x143, 0xC>(incl);                  // lane 31, to the upper half
     if (lane == 63) scratch[wave] = incl;
     __syncthreads();
-    uint32_t before = 0;
+    uint32_t part[WAVES], before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) part[w] = scratch[w];
     total = 0;
-    for (uint32_t w = 0; w < n_waves; ++w) {
-        if (w == wave) before = total;
-        total += scratch[w];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        before += uint32_t(w) < wave ? part[w] : 0;
+        total += part[w];
     }
-    __syncthreads();
     return before + incl - v;
 }
 
 // From the experts' counts: where their rows begin (each at a multiple of align), the rows of no pair marked.  The whole
 // workgroup calls it; start[e] holds expert e's count and receives its first row.  Only the workgroup that is asked to writes what
 // the caller gets.
+template <int WAVES>
 __device__ __forceinline__ void place_experts(const SortArgs& a, uint32_t* start, uint32_t* scratch, bool write) {
-    const uint32_t per = (a.E + blockDim.x - 1) / blockDim.x, e0 = threadIdx.x * per;
+    const uint32_t per = (a.E + WAVES * 64 - 1) / (WAVES * 64), e0 = threadIdx.x * per, e1 = min(e0 + per, a.E);
+    auto pad = [&](uint32_t n) { return a.align == 1 ? n : (n + a.align - 1) / a.align * a.align; };
     uint32_t sum = 0, total;
-    for (uint32_t e = e0; e < min(e0 + per, a.E); ++e) sum += (start[e] + a.align - 1) / a.align * a.align;
-    uint32_t at = exclusive_scan(sum, scratch, total);
-    for (uint32_t e = e0; e < min(e0 + per, a.E); ++e) {
-        const uint32_t n = start[e], padded = (n + a.align - 1) / a.align * a.align;
+    for (uint32_t e = e0; e < e1; ++e) sum += pad(start[e]);
+    uint32_t at = exclusive_scan<WAVES>(sum, scratch, total);
+    for (uint32_t e = e0; e < e1; ++e) {
+        const uint32_t n = start[e], padded = per == 1 ? sum : pad(n);
         start[e] = at;
         if (write) {
             a.offsets[e] = int32_t(at);
@@ -96,7 +109,7 @@ __device__ __forceinline__ void place_experts(const SortArgs& a, uint32_t* start
     }
     if (!write) return;
     if (threadIdx.x == 0) a.offsets[a.E] = int32_t(total);
-    for (uint32_t r = total + threadIdx.x; r < a.cap; r += blockDim.x) a.row_pair[r] = -1;
+    for (uint32_t r = total + threadIdx.x; r < a.cap; r += WAVES * 64) a.row_pair[r] = -1;
 }
 
 template <int GROUPS>
@@ -139,15 +152,16 @@ __global__ __launch_bounds__(WAVES * 64) void sort_one_kernel(SortArgs a) {
     uint32_t* start = lds + (WAVES * a.E * 2 + 3) / 4;
     uint32_t* scratch = start + a.E;
     const uint32_t wave = threadIdx.x >> 6;
+    int32_t expert[GROUPS];
+    load_experts<GROUPS>(a.ids, wave * 64 * GROUPS, a.P, a.E, expert);
     for (uint32_t i = threadIdx.x; i < (WAVES * a.E + 1) / 2; i += WAVES * 64) lds[i] = 0;
     __syncthreads();
-    int32_t expert[GROUPS];
     uint32_t rank[GROUPS];
-    rank_pairs<GROUPS>(a.ids, wave * 64 * GROUPS, a.P, a.E, hist + wave * a.E, expert, rank);
+    rank_pairs<GROUPS>(a.E, hist + wave * a.E, expert, rank);
     __syncthreads();
     for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64) start[e] = over_waves<WAVES>(hist, a.E, e);
     __syncthreads();
-    place_experts(a, start, scratch, true);
+    place_experts<WAVES>(a, start, scratch, true);
     __syncthreads();
     write_pairs<GROUPS>(a, wave * 64 * GROUPS, a.P, start, hist + wave * a.E, expert, rank);
 }
@@ -195,9 +209,9 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(SortArgs a) {
     }
 }
 
-// Up to so many counts of chunks a launch less pays (10 chunks of 512 experts 9.7 us against 10.7, 32 of 160 9.3 / 10.4, 80 of 512
-// 34 / 15).
-constexpr uint32_t kAddCounts = 8192;
+// Up to so many counts of chunks a launch less pays (16 chunks of 160 experts 8.0 us against 9.6, 32 of 160 9.6 / 10.1, 80 of 512
+// 34 / 11).
+constexpr uint32_t kAddCounts = 5120;
 
 // ... and each chunk puts its pairs in place, after it has worked out where the experts begin (the first one also writes that).
 // ADD: it adds up the counts of the chunks before it and of all itself, a launch less for reading all of them.
@@ -208,6 +222,9 @@ __global__ __launch_bounds__(WAVES * 64) void sort_place_kernel(SortArgs a) {
     uint16_t* hist = reinterpret_cast<uint16_t*>(lds);
     uint32_t* start = lds + (WAVES * a.E * 2 + 3) / 4;
     const uint32_t wave = threadIdx.x >> 6;
+    const uint32_t chunk = blockIdx.x * kSortChunkPairs, end = min(chunk + kSortChunkPairs, a.P), first = chunk + wave * 64 * GROUPS;
+    int32_t expert[GROUPS];
+    load_experts<GROUPS>(a.ids, first, end, a.E, expert);
     for (uint32_t i = threadIdx.x; i < (WAVES * a.E + 1) / 2; i += WAVES * 64) lds[i] = 0;
     uint32_t* before = start + a.E;                      // ADD only
     uint32_t* scratch = ADD ? before + a.E : before;
@@ -227,15 +244,13 @@ __global__ __launch_bounds__(WAVES * 64) void sort_place_kernel(SortArgs a) {
         for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64) start[e] = uint32_t(a.counts[e]);
     }
     __syncthreads();
-    place_experts(a, start, scratch, blockIdx.x == 0);
+    place_experts<WAVES>(a, start, scratch, blockIdx.x == 0);
     __syncthreads();
     for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64)
         start[e] += ADD ? before[e] : uint32_t(a.chunk_count[uint64_t(blockIdx.x) * a.E + e]);
     __syncthreads();
-    const uint32_t chunk = blockIdx.x * kSortChunkPairs, end = min(chunk + kSortChunkPairs, a.P), first = chunk + wave * 64 * GROUPS;
-    int32_t expert[GROUPS];
     uint32_t rank[GROUPS];
-    rank_pairs<GROUPS>(a.ids, first, end, a.E, hist + wave * a.E, expert, rank);
+    rank_pairs<GROUPS>(a.E, hist + wave * a.E, expert, rank);
     __syncthreads();
     for (uint32_t e = threadIdx.x; e < a.E; e += WAVES * 64) (void)over_waves<WAVES>(hist, a.E, e);
     __syncthreads();
@@ -529,6 +544,7 @@ hipError_t launch_sort(const SortArgs& a, hipStream_t stream) {
         if (a.P <= 256) return go_sort_one<4, 1>(a, stream);
         if (a.E > 1024) return go_sort_one<4, 16>(a, stream);
         if (a.P <= 1024) return go_sort_one<16, 1>(a, stream);
+        if (a.P <= 2048) return go_sort_one<16, 2>(a, stream);
         return go_sort_one<16, 4>(a, stream);
     }
     hipLaunchKernelGGL(sort_count_kernel, dim3(a.n_chunks), dim3(256), a.E * 4, stream, a);
