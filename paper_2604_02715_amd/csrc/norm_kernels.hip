@@ -264,8 +264,11 @@ __device__ __forceinline__ float* partial_row(const NormArgs& a, uint32_t sum, u
     return a.partials + (uint64_t(sum) * a.n_partials + part) * a.H;
 }
 
-template <typename Y, typename R, Mode MODE, bool D_OUT>
-__global__ __launch_bounds__(1024) void norm_grad_kernel(NormArgs a, uint32_t waves, uint32_t rows_per_wg) {
+// WAVES: the most wavefronts of a workgroup, 8 or 16.  With FP32 rows no more than 8 run on a CU where a row needs no more, and
+// each lane may have 256 registers: within the 128 of 16 wavefronts the form with all its parts spills (20480 x 2048 FP32 151 us,
+// spilling 175).  BF16 rows fit 128, and are faster compiled for them (10240 x 4096 89 us, compiled for 256 98).
+template <typename Y, typename R, Mode MODE, bool D_OUT, int WAVES>
+__global__ __launch_bounds__((kPiece<Y, R> == 8 ? 1024 : WAVES * 64)) void norm_grad_kernel(NormArgs a, uint32_t waves, uint32_t rows_per_wg) {
     typedef GradRow<Y, R, MODE, D_OUT> Row;
     constexpr int N = Row::N, P = Row::P;
     constexpr bool FACTORS = MODE == kScaled || MODE == kPost;
@@ -352,8 +355,8 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(NormArgs a, uint32_t wa
         }
     }
     // the sums of the rows side by side in a workgroup become one, by way of LDS and in their order
-    __shared__ float s_sum[2][2048];                     // [row][column]: 4 rows of up to 512, or 2 of up to 1024
-    if (rows_per_wg > 1) {
+    __shared__ float s_sum[2][WAVES == 8 ? 2048 : 1];    // [row][column]: 4 rows of up to 512, or 2 of up to 1024
+    if (WAVES == 8 && rows_per_wg > 1) {
         if (mine > 0) {
 #pragma unroll
             for (int p = 0; p < P; ++p)
@@ -519,13 +522,18 @@ hipError_t go(const NormArgs& a, bool vec, hipStream_t stream) {
     return hipGetLastError();
 }
 
+template <typename Y, typename R, Mode MODE, bool D_OUT>
+void go_grad_rows(const NormArgs& a, const RowShape& s, hipStream_t stream) {
+    if (s.waves <= 8) hipLaunchKernelGGL((norm_grad_kernel<Y, R, MODE, D_OUT, 8>), dim3(a.n_partials), dim3(s.threads()), 0, stream, a, s.waves, s.rows_per_wg);
+    else hipLaunchKernelGGL((norm_grad_kernel<Y, R, MODE, D_OUT, 16>), dim3(a.n_partials), dim3(s.threads()), 0, stream, a, s.waves, s.rows_per_wg);
+}
+
 template <typename Y, typename R, Mode MODE>
 void go_grad_rows(NormArgs& a, hipStream_t stream) {
     const RowShape s = row_shape(a.H);
-    const uint32_t wgs = walkers(s, a.T, grad_waves<Y, R>(a.H));
-    a.n_partials = wgs;
-    if (a.d_residual_out) hipLaunchKernelGGL((norm_grad_kernel<Y, R, MODE, true>), dim3(wgs), dim3(s.threads()), 0, stream, a, s.waves, s.rows_per_wg);
-    else hipLaunchKernelGGL((norm_grad_kernel<Y, R, MODE, false>), dim3(wgs), dim3(s.threads()), 0, stream, a, s.waves, s.rows_per_wg);
+    a.n_partials = walkers(s, a.T, grad_waves<Y, R>(a.H));
+    if (a.d_residual_out) go_grad_rows<Y, R, MODE, true>(a, s, stream);
+    else go_grad_rows<Y, R, MODE, false>(a, s, stream);
 }
 
 template <typename Y, typename R>
