@@ -316,10 +316,11 @@ __global__ __launch_bounds__((kPiece<Y, R> == 8 ? 1024 : WAVES * 64)) void norm_
             v[0] = two[0];
             v[1] = two[1];
         }
-        const float rstd = rstd_of(a, v[0]), mean = v[1] * rstd * inv_h;
-        const float rstd_y = MODE == kPost ? rstd_of(a, v[5]) : 1.0f;
+        const bool here = t < a.T;                       // a row that is not there adds 0, also where eps is 0
+        const float rstd = here ? rstd_of(a, v[0]) : 0.0f, mean = v[1] * rstd * inv_h;
+        const float rstd_y = MODE != kPost ? 1.0f : here ? rstd_of(a, v[5]) : 0.0f;
         float scale = a.scale;
-        if (MODE != kAlone && a.gate_token) scale *= gate_value(a, scalar_at(a.gate, min(t, a.T - 1)));
+        if (MODE != kAlone && a.gate_token) scale = here ? scale * gate_value(a, scalar_at(a.gate, min(t, a.T - 1))) : 0.0f;
         const float dot = (v[2] + rstd * (v[3] - rstd * mean * v[4])) * rstd_y;             // sum dr w_post g_channel hy
         const float mean_y = MODE == kPost ? scale * dot * inv_h : 0.0f;                     // mean(dy' w_post hy)
         float dr[P][N], dy[P][N];
@@ -341,7 +342,7 @@ __global__ __launch_bounds__((kPiece<Y, R> == 8 ? 1024 : WAVES * 64)) void norm_
                 }
             }
         next.arrive();
-        const uint32_t columns = t < a.T ? a.H : 0;
+        const uint32_t columns = here ? a.H : 0;
         const row_t r_out = row_at(static_cast<R*>(a.d_residual), t, a.d_residual_stride, columns);
         const row_t y_out = row_at(static_cast<Y*>(a.d_y), t, a.d_y_stride, columns);
 #pragma unroll
@@ -351,7 +352,7 @@ __global__ __launch_bounds__((kPiece<Y, R> == 8 ? 1024 : WAVES * 64)) void norm_
         }
         if ((MODE == kAdd || MODE == kPost) && a.gate_token) {
             const float g = a.gate_sigmoid ? gate_value(a, scalar_at(a.gate, min(t, a.T - 1))) : 0.0f;
-            if (c[0] == 0 && t < a.T) a.d_gate[t] = a.scale * dot * (a.gate_sigmoid ? g * (1.0f - g) : 1.0f);
+            if (c[0] == 0 && here) a.d_gate[t] = a.scale * dot * (a.gate_sigmoid ? g * (1.0f - g) : 1.0f);
         }
     }
     // the sums of the rows side by side in a workgroup become one, by way of LDS and in their order

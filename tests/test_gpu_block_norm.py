@@ -214,6 +214,31 @@ def test_no_tokens():
     assert d_w.abs().sum().item() == 0.0                     # a sum over no tokens
 
 
+@pytest.mark.parametrize("T,H", [(1, 64), (5, 256), (3, 1000), (2, 4096)])
+@pytest.mark.parametrize("gate,post", [(None, False), ("token", True), ("channel", True)])
+def test_eps_of_zero(T, H, gate, post):
+    """A workgroup's places without a row add nothing to the sums over the tokens, though the root of their mean square is 0."""
+    d = make(T, H, "f32", "f32", "f32", gate, post, T)
+    d = {k: (None if v is None else v + 0.01 + 0.1 * (v == 0)) for k, v in d.items()}           # no empty rows
+    g = torch.Generator().manual_seed(H)
+    d_n, d_r = torch.randn(T, H, generator=g).to(torch.bfloat16), torch.randn(T, H, generator=g)
+    got = {}
+    for eps in (0.0, 1e-12):
+        dev = {k: cuda(v) for k, v in d.items()}
+        out = {k: None if v is None else torch.full_like(cuda(v), math.nan) for k, v in d.items()}
+        ws = torch.full((M.block_norm_grad_workspace_bytes(T, H),), 0xFF, dtype=torch.uint8, device="cuda")
+        M.block_norm_grad(dev["residual"], dev["w_pre"], d_n.cuda(), out["residual"], out["w_pre"], ws, d_residual_out=d_r.cuda(), y=dev["y"],
+                          gate=dev["gate"], w_post=dev["w_post"], d_y=out["y"], d_gate=out["gate"], d_w_post=out["w_post"], eps=eps)
+        r, n = torch.empty(T, H, device="cuda"), torch.empty(T, H, dtype=torch.bfloat16, device="cuda")
+        M.block_norm(dev["residual"], dev["w_pre"], n, y=dev["y"], gate=dev["gate"], w_post=dev["w_post"], residual_out=r, eps=eps)
+        got[eps] = dict(out, r=r, n=n)
+    for k, v in got[0.0].items():
+        if v is not None:
+            # 1e-12 beside a mean square above 1e-4 moves nothing by more than 1e-8, less than a rounding
+            assert bool(torch.isfinite(v).all()), k
+            assert bool(((v.float() - got[1e-12][k].float()).abs() <= 2.0 ** -7 * v.float().abs() + 1e-5).all()), k
+
+
 def test_infinities_stay_in_their_row():
     T, H = 6, 512
     d = {k: cuda(v) for k, v in make(T, H, "f32", "f32", "f32", None, False, 1).items()}
