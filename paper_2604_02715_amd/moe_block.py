@@ -48,7 +48,11 @@ def _matrix(t, name, rows, cols, device, dtype=None):
     step, element = t.stride()
     if element != 1 and cols > 1:
         _fail("the elements of a row of %s must lie next to each other" % name)
-    return step if rows > 1 else cols
+    if rows <= 1:
+        return cols
+    if step < cols:                      # an expanded row: the norms' call takes a stride of 0 for the width
+        _fail("the rows of %s overlap (stride %d)" % (name, step))
+    return step
 
 
 def _whole(t, name, shape, dtype, device):

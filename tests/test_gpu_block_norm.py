@@ -277,3 +277,13 @@ def test_the_same_call_gives_the_same_bits_on_any_stream():
             again = run_gradient(d, dn, dr, 0.7, True, False)
         s.synchronize()
         assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+@pytest.mark.parametrize("name", ["residual", "y", "residual_out", "normed"])
+def test_expanded_rows_are_refused(name):
+    T, H = 4, 64
+    t = {k: torch.zeros(T, H, device="cuda") for k in ("residual", "y", "residual_out")}
+    t["normed"] = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    t[name] = t[name][:1].expand(T, H)
+    with pytest.raises(ValueError, match="rows of %s overlap" % name):
+        M.block_norm(t["residual"], torch.zeros(H, device="cuda"), t["normed"], y=t["y"], residual_out=t["residual_out"])

@@ -157,3 +157,15 @@ def test_tensors_are_checked_before_the_library_is_called():
                  lambda: M.block_norm(x, x[0], x)):
         with pytest.raises(ValueError, match="must be on the current GPU"):
             call()
+
+
+@pytest.mark.parametrize("rows,fine", [(1, True), (2, False), (4, False)])
+def test_rows_that_overlap(rows, fine):
+    """The norms' call takes a stride of 0 for the width: a row expanded over the tokens has it, too, and no such rows behind it."""
+    expanded = torch.zeros(1, 8).expand(rows, 8)
+    if fine:
+        assert M._matrix(expanded, "y", rows, 8, -1) == 8
+    else:
+        for t in (expanded, torch.zeros(64).as_strided((rows, 8), (4, 1))):
+            with pytest.raises(ValueError, match="overlap"):
+                M._matrix(t, "y", rows, 8, -1)
