@@ -57,6 +57,7 @@ int norm_args(const fluxmoe_norm_desc* d, uint32_t T, const void* y, const void*
     if (int rc = check_hidden(d->hidden)) return rc;
     if (!known(d->y_type) || !known(d->residual_type) || !known(d->weight_type)) return set_error(FLUXMOE_EINVAL, "unknown element type");
     const uint32_t all = FLUXMOE_NORM_GATE_TOKEN | FLUXMOE_NORM_GATE_CHANNEL | FLUXMOE_NORM_GATE_SIGMOID | FLUXMOE_NORM_ZERO_CENTRED;
+    if (d->reserved) return set_error(FLUXMOE_EINVAL, "reserved must be 0");
     if (d->flags & ~all) return set_error(FLUXMOE_EINVAL, "unknown flags 0x%x", d->flags);
     const uint32_t kind = d->flags & (FLUXMOE_NORM_GATE_TOKEN | FLUXMOE_NORM_GATE_CHANNEL);
     if (kind == (FLUXMOE_NORM_GATE_TOKEN | FLUXMOE_NORM_GATE_CHANNEL)) return set_error(FLUXMOE_EINVAL, "a gate is either the token's or the channels'");

@@ -258,18 +258,21 @@ __global__ __launch_bounds__(WAVES * 64) void sort_place_kernel(SortArgs a) {
 }
 
 // ================================================================ rows
-// Rows past the tokens: a workgroup behind the tokens' ones looks through kRowsPerPadGroup rows and clears those of no pair.
-constexpr uint32_t kRowsPerPadGroup = 16;
+// Rows past the tokens: a workgroup behind the tokens' ones looks through kRowsPerPadGroup rows and clears those of no pair, and
+// goes on to further ones where there are more than kMostPadGroups times that (a launch has fewer than 2^32 threads).
+constexpr uint32_t kRowsPerPadGroup = 16, kMostPadGroups = 1u << 20;
 
 template <typename E>      // E: what is cleared at once (16 bytes, or an element)
-__device__ __forceinline__ void clear_pad_rows(const int32_t* row_pair, uint32_t cap, uint32_t group, char* rows, uint64_t row_bytes_apart,
+__device__ __forceinline__ void clear_pad_rows(const int32_t* row_pair, uint32_t cap, uint32_t token_wgs, char* rows, uint64_t row_bytes_apart,
                                                uint32_t row_bytes) {
-    const uint32_t first = group * kRowsPerPadGroup, lane = threadIdx.x & 63;
-    uint64_t pads = __ballot(lane < kRowsPerPadGroup && first + lane < cap && row_pair[min(first + lane, cap - 1)] < 0);
-    for (; pads; pads &= pads - 1) {
-        const uint64_t r = first + __builtin_ctzll(pads);
-        E* dst = reinterpret_cast<E*>(rows + r * row_bytes_apart);
-        for (uint32_t i = threadIdx.x; i < row_bytes / sizeof(E); i += blockDim.x) dst[i] = E{};
+    const uint32_t lane = threadIdx.x & 63, step = (gridDim.x - token_wgs) * kRowsPerPadGroup;
+    for (uint32_t first = (blockIdx.x - token_wgs) * kRowsPerPadGroup; first < cap; first += step) {
+        uint64_t pads = __ballot(lane < kRowsPerPadGroup && first + lane < cap && row_pair[min(first + lane, cap - 1)] < 0);
+        for (; pads; pads &= pads - 1) {
+            const uint64_t r = first + __builtin_ctzll(pads);
+            E* dst = reinterpret_cast<E*>(rows + r * row_bytes_apart);
+            for (uint32_t i = threadIdx.x; i < row_bytes / sizeof(E); i += blockDim.x) dst[i] = E{};
+        }
     }
 }
 
@@ -283,7 +286,7 @@ RowPlan row_plan(uint32_t T, uint32_t cap, uint32_t units) {
     p.rows_per_wg = waves >= 3 ? 1 : 4 / waves;
     p.threads = 64 * waves * p.rows_per_wg;
     p.token_wgs = (T + p.rows_per_wg - 1) / p.rows_per_wg;
-    p.pad_wgs = (cap + kRowsPerPadGroup - 1) / kRowsPerPadGroup;
+    p.pad_wgs = std::min((cap + kRowsPerPadGroup - 1) / kRowsPerPadGroup, kMostPadGroups);
     return p;
 }
 
@@ -300,7 +303,7 @@ __global__ __launch_bounds__(1024) void dispatch_kernel(RowsArgs a, uint32_t ele
     char* rows = static_cast<char*>(a.rows_out);
     const uint64_t apart = a.out_stride * elem_bytes;
     if (blockIdx.x >= token_wgs) {
-        clear_pad_rows<E>(a.row_pair, a.cap, blockIdx.x - token_wgs, rows, apart, row_bytes);
+        clear_pad_rows<E>(a.row_pair, a.cap, token_wgs, rows, apart, row_bytes);
         return;
     }
     const uint32_t per_row = blockDim.x / rows_per_wg;
@@ -396,7 +399,7 @@ __global__ __launch_bounds__(1024) void combine_grad_kernel(RowsArgs a, uint32_t
     __shared__ float s_dot[16][kRouteMaxTopK];           // the wavefronts' parts of the K products
     R* d_rows = static_cast<R*>(a.rows_out);
     if (blockIdx.x >= token_wgs) {
-        clear_pad_rows<uint4>(a.row_pair, a.cap, blockIdx.x - token_wgs, static_cast<char*>(a.rows_out), a.out_stride * sizeof(R), a.H * sizeof(R));
+        clear_pad_rows<uint4>(a.row_pair, a.cap, token_wgs, static_cast<char*>(a.rows_out), a.out_stride * sizeof(R), a.H * sizeof(R));
         return;
     }
     const uint32_t per_row = blockDim.x / rows_per_wg, waves = per_row / 64;
@@ -470,7 +473,7 @@ __global__ __launch_bounds__(1024) void combine_grad_any_kernel(RowsArgs a, uint
     __shared__ float s_dot[16][kRouteMaxTopK];
     R* d_rows = static_cast<R*>(a.rows_out);
     if (blockIdx.x >= token_wgs) {
-        clear_pad_rows<R>(a.row_pair, a.cap, blockIdx.x - token_wgs, static_cast<char*>(a.rows_out), a.out_stride * sizeof(R), a.H * sizeof(R));
+        clear_pad_rows<R>(a.row_pair, a.cap, token_wgs, static_cast<char*>(a.rows_out), a.out_stride * sizeof(R), a.H * sizeof(R));
         return;
     }
     const uint32_t t = blockIdx.x;

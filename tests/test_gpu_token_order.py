@@ -244,3 +244,22 @@ def test_the_same_call_gives_the_same_bits_on_any_stream():
         assert all(torch.equal(first[k], again[k]) for k in first)
     for other in outs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
+
+
+@pytest.mark.parametrize("H", [1, 8])
+def test_more_empty_rows_than_a_launch_has_workgroups_for(H):
+    """16 rows to each of 2^20 workgroups, and some more; a column at a time and 16 bytes at a time."""
+    T, cap = 3, (1 << 24) + 1000
+    row_pair = torch.full((cap,), -1, dtype=torch.int32, device="cuda")
+    pair_row = torch.tensor([[5], [cap - 2], [(1 << 24) + 7]], dtype=torch.int32, device="cuda")
+    row_pair[pair_row.flatten().long()] = torch.arange(T, dtype=torch.int32, device="cuda")
+    x = torch.randn(T, H, device="cuda").to(torch.bfloat16)
+    rows = torch.full((cap, H), 7.0, dtype=torch.bfloat16, device="cuda")
+    M.dispatch(x, pair_row, row_pair, rows)
+    want = torch.zeros_like(rows)
+    want[pair_row.flatten().long()] = x
+    assert torch.equal(rows, want)
+    d_rows, d_gates = torch.full_like(rows, 7.0), torch.empty(T, 1, device="cuda")
+    M.combine_grad(x, rows, pair_row, row_pair, torch.ones(T, 1, device="cuda"), d_rows, d_gates)
+    assert torch.equal(d_rows, want)
+    assert torch.allclose(d_gates[:, 0], x.float().square().sum(1), rtol=1e-6)

@@ -159,6 +159,10 @@ def test_tensors_are_checked_before_the_library_is_called():
             call()
 
 
+def test_norm_refuses_a_reserved_field():
+    refused(-1, norm, B.NormDesc(64, B.F32, B.F32, B.F32, 0, 1e-6, 1.0, 1))
+
+
 @pytest.mark.parametrize("rows,fine", [(1, True), (2, False), (4, False)])
 def test_rows_that_overlap(rows, fine):
     """The norms' call takes a stride of 0 for the width: a row expanded over the tokens has it, too, and no such rows behind it."""
