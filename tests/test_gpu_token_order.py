@@ -263,3 +263,19 @@ def test_more_empty_rows_than_a_launch_has_workgroups_for(H):
     M.combine_grad(x, rows, pair_row, row_pair, torch.ones(T, 1, device="cuda"), d_rows, d_gates)
     assert torch.equal(d_rows, want)
     assert torch.allclose(d_gates[:, 0], x.float().square().sum(1), rtol=1e-6)
+
+
+@pytest.mark.parametrize("T,K,E", [(3, 2, 8), (100, 10, 512), (300, 8, 160), (3000, 3, 9), (6000, 10, 512)])
+@pytest.mark.parametrize("align,first,more", [(1, 1, 0), (128, 1, 2), (128, 2, 5), (100, 3, 3), (1024, 0, 1)])
+def test_rows_of_no_pair(T, K, E, align, first, more):
+    """Long gaps between the groups; row_pair at any 4-byte address and of any length, and nothing beside it is written."""
+    ids = make_ids(T, K, E, 3, 0.1)
+    cap = M.sorted_rows(T, K, E, align) + more
+    i32 = dict(dtype=torch.int32, device="cuda")
+    whole = torch.full((first + cap + 8,), -9, **i32)
+    row_pair = whole[first:first + cap]
+    o = [torch.empty(E + 1, **i32), torch.empty(E, **i32), torch.empty(T, K, **i32), row_pair]
+    M.sort_tokens(ids.cuda(), E, *o, torch.empty(M.sort_workspace_bytes(T, K, E), dtype=torch.uint8, device="cuda"), align=align)
+    for got, want in zip(o, plain_order(ids, E, align, cap)):
+        assert got.reshape(-1).cpu().tolist() == want
+    assert bool((whole[:first] == -9).all()) and bool((whole[first + cap:] == -9).all())
