@@ -87,16 +87,19 @@ __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* scratch
     return before + incl - v;
 }
 
-// All rows without a pair, before the pairs get theirs: neighbouring threads write neighbouring rows, where each expert's thread
-// marking what its group is short of a multiple of `align` took 37 us for 400 x 10 of 512 at 128 (now 9).
-__device__ __forceinline__ void clear_rows(const SortArgs& a, uint32_t thread, uint32_t threads) {
+// Rows first .. cap - 1 without a pair, by neighbouring threads.  Where groups have gaps this goes over all rows before the pairs get
+// theirs (each expert's thread marking its own gap took 37 us for 400 x 10 of 512 at 128, this 9); at align 1 only the rows past
+// the last group are marked, when that is known (8192 x 2 of 8 and the rows' copy 36.5 us, 37.3 with all rows marked first).
+__device__ __forceinline__ void clear_rows(const SortArgs& a, uint32_t first, uint32_t thread, uint32_t threads) {
     typedef int32_t four __attribute__((ext_vector_type(4), aligned(4)));
-    for (uint32_t i = thread; i < a.cap / 4; i += threads) *reinterpret_cast<four*>(a.row_pair + uint64_t(i) * 4) = four{-1, -1, -1, -1};
-    if (thread < a.cap % 4) a.row_pair[a.cap - 1 - thread] = -1;
+    const uint32_t n = a.cap - first;
+    int32_t* rows = a.row_pair + first;
+    for (uint32_t i = thread; i < n / 4; i += threads) *reinterpret_cast<four*>(rows + uint64_t(i) * 4) = four{-1, -1, -1, -1};
+    if (thread < n % 4) rows[n - 1 - thread] = -1;
 }
 
 // From the experts' counts: where their rows begin (each at a multiple of align).  The whole workgroup calls it; start[e] holds
-// expert e's count and receives its first row.  Only the workgroup that is asked to writes what the caller gets.
+// expert e's count and receives its first row.  Only the workgroup that is asked to writes offsets and counts.
 template <int WAVES>
 __device__ __forceinline__ void place_experts(const SortArgs& a, uint32_t* start, uint32_t* scratch, bool write) {
     const uint32_t per = (a.E + WAVES * 64 - 1) / (WAVES * 64), e0 = threadIdx.x * per, e1 = min(e0 + per, a.E);
@@ -114,6 +117,7 @@ __device__ __forceinline__ void place_experts(const SortArgs& a, uint32_t* start
         at += padded;
     }
     if (write && threadIdx.x == 0) a.offsets[a.E] = int32_t(total);
+    if (a.align == 1) clear_rows(a, total, blockIdx.x * (WAVES * 64) + threadIdx.x, gridDim.x * (WAVES * 64));
 }
 
 template <int GROUPS>
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(WAVES * 64) void sort_one_kernel(SortArgs a) {
     uint32_t* scratch = start + a.E;
     const uint32_t wave = threadIdx.x >> 6;
     int32_t expert[GROUPS];
-    clear_rows(a, threadIdx.x, WAVES * 64);
+    if (a.align != 1) clear_rows(a, 0, threadIdx.x, WAVES * 64);
     load_experts<GROUPS>(a.ids, wave * 64 * GROUPS, a.P, a.E, expert);
     for (uint32_t i = threadIdx.x; i < (WAVES * a.E + 1) / 2; i += WAVES * 64) lds[i] = 0;
     __syncthreads();
@@ -171,11 +175,11 @@ __global__ __launch_bounds__(WAVES * 64) void sort_one_kernel(SortArgs a) {
     write_pairs<GROUPS>(a, wave * 64 * GROUPS, a.P, start, hist + wave * a.E, expert, rank);
 }
 
-// Large batches: chunks of kSortChunkPairs pairs.  First each chunk's counts (and all rows without a pair) ...
+// Large batches: chunks of kSortChunkPairs pairs.  First each chunk's counts (and where groups have gaps, all rows without a pair) ...
 __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
     extern __shared__ __align__(16) uint32_t lds[];
     for (uint32_t e = threadIdx.x; e < a.E; e += 256) lds[e] = 0;
-    clear_rows(a, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+    if (a.align != 1) clear_rows(a, 0, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
     __syncthreads();
     const uint32_t first = blockIdx.x * kSortChunkPairs, end = min(first + kSortChunkPairs, a.P);
     for (uint32_t p = first + threadIdx.x; p < end; p += 256) {
