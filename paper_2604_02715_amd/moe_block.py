@@ -187,7 +187,7 @@ def combine_grad(d_out, rows, pair_row, row_pair, gates, d_rows, d_gates, *, str
 # ------------------------------------------------------------------------------------------ norms around a block
 @functools.lru_cache(maxsize=256)
 def _norm_desc(*fields):
-    """The argument block of a kind of call: sizes, types and constants, nothing of its tensors."""
+    """The argument block of a kind of call: sizes, types and constants as plain numbers, nothing of its tensors."""
     return ctypes.pointer(B.NormDesc(*fields))
 
 
@@ -226,7 +226,8 @@ def block_norm(residual, w_pre, normed, *, y=None, gate=None, w_post=None, resid
     if y is not None:
         y_stride, y_type = _matrix(y, "y", T, H, device), _TYPES[y.dtype]
         o_stride = _matrix(residual_out, "residual_out", T, H, device, residual.dtype)
-    desc = _norm_desc(H, y_type, _TYPES[residual.dtype], _TYPES[w_pre.dtype], flags, eps, scale, 0, y_stride, r_stride, o_stride, n_stride)
+    desc = _norm_desc(H, y_type, _TYPES[residual.dtype], _TYPES[w_pre.dtype], flags, float(eps), float(scale), 0, y_stride, r_stride,
+                      o_stride, n_stride)
     B.fluxmoe_block_norm(desc, T, _ptr(y), residual.data_ptr(), _ptr(gate), _ptr(w_post), w_pre.data_ptr(), _ptr(residual_out),
                          normed.data_ptr(), _sptr(stream, device))
 
@@ -258,8 +259,8 @@ def block_norm_grad(residual_out, w_pre, d_normed, d_residual, d_w_pre, workspac
     if d_gate is not None:
         _whole(d_gate, "d_gate", tuple(gate.shape), torch.float32, device)
     _whole(workspace, "workspace", (workspace.numel(),), torch.uint8, device)
-    desc = _norm_desc(H, y_type, _TYPES[rt], _TYPES[w_pre.dtype], flags, eps, scale, 0, y_stride, 0, o_stride, 0, dy_stride, dr_stride,
-                      do_stride, dn_stride)
+    desc = _norm_desc(H, y_type, _TYPES[rt], _TYPES[w_pre.dtype], flags, float(eps), float(scale), 0, y_stride, 0, o_stride,
+                      0, dy_stride, dr_stride, do_stride, dn_stride)
     B.fluxmoe_block_norm_grad(desc, T, _ptr(y), residual_out.data_ptr(), _ptr(gate), _ptr(w_post), w_pre.data_ptr(), _ptr(d_residual_out),
                               d_normed.data_ptr(), d_residual.data_ptr(), _ptr(d_y), _ptr(d_gate), _ptr(d_w_post), d_w_pre.data_ptr(),
                               workspace.data_ptr(), workspace.numel(), _sptr(stream, device))
