@@ -72,6 +72,13 @@ __device__ __forceinline__ void weights_at(const NormArgs& a, const void* w, uin
     }
 }
 __device__ __forceinline__ float gate_value(const NormArgs& a, float v) { return a.gate_sigmoid ? sigmoid(v) : v; }
+// The gate's derivative by what is read: a sigmoid's by e = e^-|v|, as 1 - g of a rounded g has three digits left at v = 10 and none
+// from 17 on.
+__device__ __forceinline__ float gate_slope(const NormArgs& a, float v) {
+    if (!a.gate_sigmoid) return 1.0f;
+    const float e = expf(-fabsf(v)), one_e = 1.0f + e;
+    return e / (one_e * one_e);
+}
 template <int N>
 __device__ __forceinline__ void gates_at(const NormArgs& a, uint32_t c, float* f) {
     Pack<float, N> p;
@@ -351,8 +358,8 @@ __global__ __launch_bounds__((kPiece<Y, R> == 8 ? 1024 : WAVES * 64)) void norm_
             if (MODE != kAlone) store<Y, N, kStream>(y_out, c[p], dy[p]);
         }
         if ((MODE == kAdd || MODE == kPost) && a.gate_token) {
-            const float g = a.gate_sigmoid ? gate_value(a, scalar_at(a.gate, min(t, a.T - 1))) : 0.0f;
-            if (c[0] == 0 && here) a.d_gate[t] = a.scale * dot * (a.gate_sigmoid ? g * (1.0f - g) : 1.0f);
+            const float v_gate = scalar_at(a.gate, min(t, a.T - 1));
+            if (c[0] == 0 && here) a.d_gate[t] = a.scale * dot * gate_slope(a, v_gate);
         }
     }
     // the sums of the rows side by side in a workgroup become one, by way of LDS and in their order
@@ -415,7 +422,7 @@ __global__ __launch_bounds__(1024) void norm_grad_any_kernel(NormArgs a) {
         row_sums<3>(v, s_a, waves);
         const float rstd = rstd_of(a, v[0]), mean = v[1] * rstd * inv_h;
         const float rstd_y = a.w_post ? rstd_of(a, v[2]) : 1.0f;
-        const float g_token = a.gate_token ? gate_value(a, a.gate[t]) : 1.0f, scale = a.scale * g_token;
+        const float scale = a.gate_token ? a.scale * gate_value(a, a.gate[t]) : a.scale;
         auto dr_at = [&](uint32_t c) {
             const float h = to_float(r[c]) * rstd;
             return (a.d_residual_out ? to_float(d_out[c]) : 0.0f) + rstd * (to_float(dn[c]) * weight_at(a, a.w_pre, c) - h * mean);
@@ -441,7 +448,7 @@ __global__ __launch_bounds__(1024) void norm_grad_any_kernel(NormArgs a) {
             }
             from_float(static_cast<R*>(a.d_residual) + t * a.d_residual_stride + c, dr);
         }
-        if (a.gate_token && threadIdx.x == 0) a.d_gate[t] = a.scale * dot[0] * (a.gate_sigmoid ? g_token * (1.0f - g_token) : 1.0f);
+        if (a.gate_token && threadIdx.x == 0) a.d_gate[t] = a.scale * dot[0] * gate_slope(a, a.gate[t]);
         __syncthreads();
     }
 }
@@ -478,7 +485,7 @@ __global__ __launch_bounds__(256) void column_sum_kernel(NormArgs a) {
     }
     const float g = a.gate_channel ? gate_value(a, a.gate[to]) : 1.0f;
     if (a.w_post) a.d_w_post[to] = g * sum;
-    if (a.gate_channel) a.d_gate[to] = (a.w_post ? weight_at(a, a.w_post, to) : 1.0f) * sum * (a.gate_sigmoid ? g * (1.0f - g) : 1.0f);
+    if (a.gate_channel) a.d_gate[to] = (a.w_post ? weight_at(a, a.w_post, to) : 1.0f) * sum * gate_slope(a, a.gate[to]);
 }
 
 uint32_t any_threads(uint32_t H) { return H >= 1024 ? 1024 : (H + 63) / 64 * 64; }
