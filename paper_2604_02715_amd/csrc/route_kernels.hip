@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kThreads) void route_many_kernel(RouteArgs a) {
 
 // With c the chosen scores (a softmax's numerators: its sum cancels where the gates are divided by theirs), C their sum and
 // d = scale * d_gates:
-//   renormalised:  d_c = (d - sum(d c) / C) / C, then times c (softmax) or c (1 - c) (sigmoid)
+//   renormalised:  (d - sum(d c) / C) times c / C (softmax) or c (1 - c) / C (sigmoid)
 //   sigmoid:       d c (1 - c)
 //   softmax:       p_i (d_i - sum_j d_j p_j) for every expert i of the row, chosen or not
 // The K values of a row are spread over its experts in LDS; the lanes then write the row, eight experts at a time.
@@ -316,7 +316,8 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteArgs a) {
             float total = group_sum<LPR>(c);
             if (total == 0.0f) total = 1.0f;
             mean = group_sum<LPR>(chosen ? d * (c / total) : 0.0f);
-            d = (d - mean) / total;
+            d -= mean;
+            slope /= total;                              // at most 1, where 1 / total of sigmoids below the normal numbers is infinite
         }
         d *= slope;
     }
