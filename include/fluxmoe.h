@@ -444,8 +444,9 @@ int fluxmoe_balanced_split(double beta_gpu, double beta_cpu, uint32_t experts_pe
  * run elsewhere, the norms on either side of a block, and the gradients of all three.  Device pointers
  * only; no context; nothing is kept between calls and nothing allocated; the calls only enqueue on
  * `stream`, so their order with the calls above is the stream's.  T <= 2^20, E <= 4096, K <= 64, hidden <= 2^20;
- * T = 0 is valid.  Strides are in elements, from one row to the next.  Element types are FLUXMOE_BF16 or
- * FLUXMOE_F32; sums are FP32, and each output is rounded once.  The same call gives the same bits.
+ * T = 0 is valid, and pointers to what has a row for each token may be NULL then.  Strides are in elements, from
+ * one row to the next.  Element types are FLUXMOE_BF16 or FLUXMOE_F32; sums are FP32, and each output is rounded
+ * once.  The same call gives the same bits.
  * Rows at 16-byte addresses (strides too) are read 16 bytes at a time; any others an element at a time.
  * ------------------------------------------------------------------------------------------ */
 #define FLUXMOE_BF16 0u

@@ -50,6 +50,7 @@ int check_rows(uint32_t T, uint32_t K, uint32_t H, uint64_t rows_cap) {
     return FLUXMOE_OK;
 }
 
+// With T = 0 the addresses of what has a row for each token (y, a token's gate) say nothing: an empty tensor's is NULL.
 int norm_args(const fluxmoe_norm_desc* d, uint32_t T, const void* y, const void* residual, const float* gate, const void* w_post,
               const void* w_pre, NormArgs& a) {
     if (!d) return set_error(FLUXMOE_EINVAL, "desc is NULL");
@@ -61,9 +62,10 @@ int norm_args(const fluxmoe_norm_desc* d, uint32_t T, const void* y, const void*
     if (d->flags & ~all) return set_error(FLUXMOE_EINVAL, "unknown flags 0x%x", d->flags);
     const uint32_t kind = d->flags & (FLUXMOE_NORM_GATE_TOKEN | FLUXMOE_NORM_GATE_CHANNEL);
     if (kind == (FLUXMOE_NORM_GATE_TOKEN | FLUXMOE_NORM_GATE_CHANNEL)) return set_error(FLUXMOE_EINVAL, "a gate is either the token's or the channels'");
-    if ((kind != 0) != (gate != nullptr)) return set_error(FLUXMOE_EINVAL, "the flags and the gate pointer disagree on whether there is a gate");
+    const bool told = T || kind != FLUXMOE_NORM_GATE_TOKEN;
+    if (told && (kind != 0) != (gate != nullptr)) return set_error(FLUXMOE_EINVAL, "the flags and the gate pointer disagree on whether there is a gate");
     if ((d->flags & FLUXMOE_NORM_GATE_SIGMOID) && !kind) return set_error(FLUXMOE_EINVAL, "FLUXMOE_NORM_GATE_SIGMOID without a gate");
-    if (!y && (gate || w_post)) return set_error(FLUXMOE_EINVAL, "a gate or w_post without y");
+    if (T && !y && (gate || w_post)) return set_error(FLUXMOE_EINVAL, "a gate or w_post without y");
     if (!(d->eps >= 0.0f)) return set_error(FLUXMOE_EINVAL, "eps must not be negative");
     a = NormArgs{};
     a.T = T;
@@ -319,10 +321,11 @@ int fluxmoe_block_norm_grad(const fluxmoe_norm_desc* d, uint32_t T, const void* 
                             void* stream) {
     NormArgs a;
     if (int rc = norm_args(d, T, y, residual_out, gate, w_post, w_pre, a)) return rc;
-    if ((d_w_post != nullptr) != (w_post != nullptr) || (d_gate != nullptr) != (gate != nullptr) || (d_y != nullptr) != (y != nullptr))
+    if ((d_w_post != nullptr) != (w_post != nullptr) || ((T || a.gate_channel) && (d_gate != nullptr) != (gate != nullptr)) ||
+        (T && (d_y != nullptr) != (y != nullptr)))
         return set_error(FLUXMOE_EINVAL, "d_y, d_gate and d_w_post go with y, gate and w_post");
     if (!d_w_pre || !w_pre || (T && (!residual_out || !d_normed || !d_residual))) return set_error(FLUXMOE_EINVAL, "NULL argument");
-    if ((d_residual == d_residual_out && a.d_residual_stride != a.d_residual_out_stride) || (d_y && d_y == y && a.d_y_stride != a.y_stride))
+    if ((T && d_residual == d_residual_out && a.d_residual_stride != a.d_residual_out_stride) || (d_y && d_y == y && a.d_y_stride != a.y_stride))
         return set_error(FLUXMOE_EINVAL, "a gradient in its input's place must have its stride");
     const uint32_t yb = elem_bytes(d->y_type), rb = elem_bytes(d->residual_type);
     if (!aligned(d_residual_out, rb) || !aligned(d_normed, 2) || !aligned(d_residual, rb) || !aligned(d_y, yb) || !aligned(d_gate, 4) ||

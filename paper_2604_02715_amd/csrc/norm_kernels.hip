@@ -546,21 +546,20 @@ void go_grad_rows(NormArgs& a, hipStream_t stream) {
 
 template <typename Y, typename R>
 hipError_t go_grad(NormArgs a, bool vec, hipStream_t stream) {
-    const Mode mode = mode_of(a);
     if (a.T == 0) {
         a.n_partials = 0;
     } else if (!vec || a.H > kRowColumns) {
         a.n_partials = a.T < 256 ? a.T : 256;
         hipLaunchKernelGGL((norm_grad_any_kernel<Y, R>), dim3(a.n_partials), dim3(any_threads(a.H)), 0, stream, a);
     } else {
-        switch (mode) {
+        switch (mode_of(a)) {
             case kAlone: go_grad_rows<R, R, kAlone>(a, stream); break;
             case kAdd: go_grad_rows<Y, R, kAdd>(a, stream); break;
             case kScaled: go_grad_rows<Y, R, kScaled>(a, stream); break;
             case kPost: go_grad_rows<Y, R, kPost>(a, stream); break;
         }
     }
-    const uint32_t n_sums = mode == kScaled || mode == kPost ? 2 : 1;
+    const uint32_t n_sums = a.w_post || a.gate_channel ? 2 : 1;          // also of no tokens, where y's address says nothing
     hipLaunchKernelGGL(column_sum_kernel, dim3((a.H + 15) / 16, n_sums), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
