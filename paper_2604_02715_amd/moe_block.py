@@ -23,6 +23,11 @@ def _fail(what):
     raise ValueError(what)
 
 
+def _too_large():
+    # a call's sizes, or-ed together, go past 32 bits (or below 0): ctypes would hand on their low half
+    _fail("a size is not from 0 to 2^32 - 1")
+
+
 def _sptr(stream, device):
     if stream is None:
         return _current_stream(device) if _current_stream else torch.cuda.current_stream(device).cuda_stream
@@ -77,6 +82,8 @@ def _logits(logits):
         _fail("logits must be [tokens][experts]")
     device = _place(logits, "logits")
     T, E = logits.shape
+    if (T | E) >> 32:
+        _too_large()
     return device, T, E, _matrix(logits, "logits", T, E, device)
 
 
@@ -86,6 +93,8 @@ def route(logits, ids, gates, *, bias=None, scale=1.0, score="softmax", renormal
     if ids.dim() != 2:
         _fail("ids must be [tokens][top_k]")
     K = ids.shape[1]
+    if K >> 32:
+        _too_large()
     _whole(ids, "ids", (T, K), torch.int32, device)
     _whole(gates, "gates", (T, K), torch.float32, device)
     if bias is not None:
@@ -100,6 +109,8 @@ def route_grad(logits, ids, d_gates, d_logits, *, scale=1.0, score="softmax", re
     if ids.dim() != 2:
         _fail("ids must be [tokens][top_k]")
     K = ids.shape[1]
+    if K >> 32:
+        _too_large()
     _whole(ids, "ids", (T, K), torch.int32, device)
     _whole(d_gates, "d_gates", (T, K), torch.float32, device)
     d_stride = _matrix(d_logits, "d_logits", T, E, device, logits.dtype)
@@ -110,10 +121,14 @@ def route_grad(logits, ids, d_gates, d_logits, *, scale=1.0, score="softmax", re
 # ------------------------------------------------------------------------------------------ tokens by expert and back
 def sorted_rows(tokens, top_k, n_experts, align=1) -> int:
     """Rows that the pairs of such a batch can take: what row_pair and the rows' matrices must hold."""
+    if (tokens | top_k | n_experts | align) >> 32:
+        _too_large()
     return B.fluxmoe_sorted_rows(tokens, top_k, n_experts, align)
 
 
 def sort_workspace_bytes(tokens, top_k, n_experts) -> int:
+    if (tokens | top_k | n_experts) >> 32:
+        _too_large()
     return B.fluxmoe_sort_workspace_bytes(tokens, top_k, n_experts)
 
 
@@ -123,6 +138,8 @@ def sort_tokens(ids, n_experts, offsets, counts, pair_row, row_pair, workspace=N
         _fail("ids must be [tokens][top_k]")
     device = _place(ids, "ids")
     T, K = ids.shape
+    if (T | K | n_experts | align) >> 32:
+        _too_large()
     _whole(ids, "ids", (T, K), torch.int32, device)
     _whole(offsets, "offsets", (n_experts + 1,), torch.int32, device)
     _whole(counts, "counts", (n_experts,), torch.int32, device)
@@ -135,10 +152,12 @@ def sort_tokens(ids, n_experts, offsets, counts, pair_row, row_pair, workspace=N
                           _sptr(stream, device))
 
 
-def _order(pair_row, row_pair, device):
+def _order(pair_row, row_pair, H, device):
     if pair_row.dim() != 2:
         _fail("pair_row must be [tokens][top_k]")
     T, K = pair_row.shape
+    if (T | K | H) >> 32:
+        _too_large()
     _whole(pair_row, "pair_row", (T, K), torch.int32, device)
     if row_pair is not None:
         _whole(row_pair, "row_pair", (row_pair.numel(),), torch.int32, device)
@@ -148,8 +167,8 @@ def _order(pair_row, row_pair, device):
 def dispatch(x, pair_row, row_pair, rows, *, stream=None):
     """rows [row_pair.numel()][H] <- x [T][H], both of one type; rows of no pair become 0."""
     device = _place(x, "x")
-    T, K = _order(pair_row, row_pair, device)
     H = x.shape[-1]
+    T, K = _order(pair_row, row_pair, H, device)
     x_stride = _matrix(x, "x", T, H, device)
     rows_stride = _matrix(rows, "rows", row_pair.numel(), H, device, x.dtype)
     B.fluxmoe_dispatch(x.data_ptr(), _TYPES[x.dtype], T, H, x_stride, pair_row.data_ptr(), K, row_pair.data_ptr(), row_pair.numel(),
@@ -159,8 +178,8 @@ def dispatch(x, pair_row, row_pair, rows, *, stream=None):
 def combine(rows, pair_row, gates, out, *, accumulate=False, stream=None):
     """out [T][H] <- sum over k of gates [T][K] (None: ones, the gradient of dispatch) times rows [n][H]."""
     device = _place(rows, "rows")
-    T, K = _order(pair_row, None, device)
     n, H = rows.shape[0], rows.shape[-1]
+    T, K = _order(pair_row, None, H, device)
     rows_stride = _matrix(rows, "rows", n, H, device)
     out_stride = _matrix(out, "out", T, H, device)
     if gates is not None:
@@ -172,8 +191,8 @@ def combine(rows, pair_row, gates, out, *, accumulate=False, stream=None):
 def combine_grad(d_out, rows, pair_row, row_pair, gates, d_rows, d_gates, *, stream=None):
     """d_rows [n][H] (the rows' type), d_gates float32 [T][K] <- d_out [T][H], and what combine was given."""
     device = _place(d_out, "d_out")
-    T, K = _order(pair_row, row_pair, device)
     n, H = row_pair.numel(), d_out.shape[-1]
+    T, K = _order(pair_row, row_pair, H, device)
     d_out_stride = _matrix(d_out, "d_out", T, H, device)
     rows_stride = _matrix(rows, "rows", n, H, device)
     d_rows_stride = _matrix(d_rows, "d_rows", n, H, device, rows.dtype)
@@ -197,6 +216,8 @@ def _norm_inputs(residual, w_pre, y, gate, w_post, gate_sigmoid, zero_centred):
     if residual.dim() != 2:
         _fail("residual must be [tokens][hidden]")
     T, H = residual.shape
+    if (T | H) >> 32:
+        _too_large()
     if w_pre.dtype not in _TYPES:
         _fail("w_pre has type %s" % w_pre.dtype)
     _whole(w_pre, "w_pre", (H,), w_pre.dtype, device)
@@ -233,6 +254,8 @@ def block_norm(residual, w_pre, normed, *, y=None, gate=None, w_post=None, resid
 
 
 def block_norm_grad_workspace_bytes(tokens, hidden) -> int:
+    if (tokens | hidden) >> 32:
+        _too_large()
     return B.fluxmoe_block_norm_grad_workspace_bytes(tokens, hidden)
 
 
