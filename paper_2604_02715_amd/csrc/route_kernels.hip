@@ -5,9 +5,9 @@
 // expert: each lane knows its best, the lanes' largest is found in log2(LPR) steps, a ballot names the lowest lane that has
 // it (its experts come before those of the others, so equal scores go to the lowest expert), and that lane alone takes the
 // expert out and looks for its next best.
-// The K rounds follow each other: bound by their length where rows are few (1 x 512 top-10 3.8 us, the launch's 2.1 included), by
-// instructions where they are many (16381 x 160 by sigmoids 8.7 us in route_many_kernel; its bytes would take 1).  The gradient is
-// bound by memory (8192 x 512 FP32, every logit, 8.1 us; bytes 5.2).
+// The K rounds follow each other: bound by their length (1 x 512 top-10 3.8 us, the launch's 2.1 included; 16381 x 160 by sigmoids
+// 8.7 us in route_many_kernel, which takes 7 from 2048 rows on, for bytes of 1), and by instructions beyond that, where there are more rows
+// than the CUs hold at once (32768 x 160 11.9).  The gradient is bound by memory (8192 x 512 FP32, every logit, 8.1 us; bytes 5.2).
 #include <cmath>
 
 #include "block_device.h"
@@ -155,9 +155,9 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     }
 }
 
-// The same for many rows, with fewer lanes to a row and so fewer instructions: 8 or 16 lanes, up to four chunks of eight experts
-// to each.  The keys lie in LDS (each lane's own), the chunks' largest ones in registers; when a lane's best is taken, only that
-// chunk is read again.  Of equal keys the largest complement of an expert's number wins.
+// The same for many rows, with fewer lanes to a row and so fewer instructions in all, if in longer rounds: 8 or 16 lanes, up to four
+// chunks of eight experts to each.  The keys lie in LDS (each lane's own), the chunks' largest ones in registers; when a lane's best is
+// taken, only that chunk is read again.  Of equal keys the largest complement of an expert's number wins.
 template <typename L, int LPR, int CHUNKS, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void route_many_kernel(RouteArgs a) {
     __shared__ uint4 s_key[CHUNKS][2][kThreads];
@@ -361,15 +361,28 @@ void go_grad(const RouteArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((route_grad_kernel<L, LPR, CHUNKS, SIGMOID>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
 }
 
-// With many rows the instructions count, and route_many_kernel has fewer; below, a round's length does (us, route_many_kernel /
-// route_kernel: 16384 x 512 top-10 11.0 / 19.5, 8192 x 512 7.5 / 11.1, 4096 x 512 7.5 / 7.1, 1 x 512 7.1 / 4.1; 16384 x 160 top-8 by
-// sigmoids 8.0 / 14.0, 8192 x 160 7.1 / 7.8, 4096 x 160 8.2 / 5.4).
-constexpr uint32_t kManyRows = 4096;
+// The rows beyond which route_many_kernel is the faster one.  Its rounds are longer, but its wavefronts hold several times as many rows,
+// so that it goes on at a chain's length (160 experts, top-8 by sigmoids: 6.9 us from 2048 to 8192 rows, 7.8 at 16384) where
+// route_kernel takes longer with the rows (4.5 at 2048, 6.4 at 6144, 7.6 at 6145, 12.2 at 16384).  Its time over route_kernel's, top-8 by
+// sigmoids (BF16) / by softmax (FP32); 16 choices cross earlier, two later:
+//   experts  4097 rows    6144         6145         8192         8193         12288
+//       128  0.95 / 1.03  0.91 / 0.95  0.81 / 0.86  0.77 / 0.82  0.75 / 0.77  0.64 / 0.66
+//       160  1.13 / 1.22  1.07 / 1.13  0.94 / 1.04  0.90 / 0.98  0.91 / 0.92  0.77 / 0.77
+//       193  1.45 / 1.35  1.35 / 1.24  1.19 / 1.16  1.11 / 1.10  1.10 / 1.06  0.93 / 1.05
+//       256  1.33 / 1.33  1.22 / 1.27  1.10 / 1.14  1.03 / 1.09  1.09 / 1.01  0.90 / 0.84
+//       384  1.07 / 1.00  0.88 / 0.84  0.85 / 0.79  0.73 / 0.70  0.87 / 0.75  0.68 / 0.62
+//       512  1.10 / 1.02  0.92 / 0.84  0.87 / 0.81  0.76 / 0.70  0.91 / 0.77  0.70 / 0.63
+//   160, 16  1.01         0.96         0.84         0.80         0.81         0.68
+//   256, 16  1.18         1.11         0.97         0.92         0.96         0.79
+//   160, 2   1.21         1.12         1.11         1.03         1.05         0.90
+//   256, 2   1.42         1.27         1.28         1.14         1.22         0.99
+// Up to 128 experts and from 257 on they are level about 4096 rows.
+uint32_t many_rows(uint32_t E) { return E <= 128 || E > 256 ? 4096 : E <= 192 ? 6144 : 8192; }
 
 // As few lanes to a row as hold its experts at eight each, and one for every chosen expert.
 template <typename L, bool SIGMOID>
 void pick(const RouteArgs& a, hipStream_t stream) {
-    if (a.T > kManyRows && a.E > 64 && a.E <= 512 && a.K <= 16) {
+    if (a.T > many_rows(a.E) && a.E > 64 && a.E <= 512 && a.K <= 16) {
         if (a.E <= 128) go_many<L, SIGMOID, 8, 2>(a, stream);
         else if (a.E <= 192) go_many<L, SIGMOID, 8, 3>(a, stream);
         else if (a.E <= 256) go_many<L, SIGMOID, 8, 4>(a, stream);
