@@ -5,9 +5,9 @@
 // expert: each lane knows its best, the lanes' largest is found in log2(LPR) steps, a ballot names the lowest lane that has
 // it (its experts come before those of the others, so equal scores go to the lowest expert), and that lane alone takes the
 // expert out and looks for its next best.
-// The K rounds follow each other: bound by their length (1 x 512 top-10 3.8 us, the launch's 2.1 included; 16381 x 160 by sigmoids
-// 8.7 us in route_many_kernel, which takes 7 from 2048 rows on, for bytes of 1), and by instructions beyond that, where there are more rows
-// than the CUs hold at once (32768 x 160 11.9).  The gradient is bound by memory (8192 x 512 FP32, every logit, 8.1 us; bytes 5.2).
+// The K rounds follow each other: bound by their length (1 x 512 top-10 4 us, the launch's 2.1 included; 16381 x 160 by sigmoids
+// 8.6 us in route_many_kernel, which takes 7 from 2048 rows on, for bytes of 1), and by instructions beyond that, where there are more rows
+// than the CUs hold at once (32768 x 160 11.9).  The gradient is bound by memory (8192 x 512 FP32, every logit, 7.9 us; bytes 5.2).
 #include <cmath>
 
 #include "block_device.h"

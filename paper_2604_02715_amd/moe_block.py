@@ -4,6 +4,10 @@ expert and back for experts that run elsewhere, the norms on either side of a bl
 Every function checks its tensors, enqueues one call of libfluxmoe.so on `stream` (default: the current one) and returns; the
 caller owns all buffers, the outputs among them, and keeps them until the work is done.  Matrices may have any row stride of at
 least a row; a row's elements lie next to each other.  What the calls compute stands in include/fluxmoe.h.
+
+The calls write into the tensors' memory and are no part of an autograd graph, also where a tensor requires a gradient: a program
+calls the gradients itself, or from a torch.autograd.Function of its own.  eps and scale are numbers; the norms take a tensor
+of one, too, and read it at the call, which waits for it where it is on the GPU.
 """
 from __future__ import annotations
 
