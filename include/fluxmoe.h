@@ -468,6 +468,18 @@ int fluxmoe_balanced_split(double beta_gpu, double beta_cpu, uint32_t experts_pe
 #define FLUXMOE_ROUTE_RENORMALIZE 2u
 int fluxmoe_route(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride, const float* bias,
                   uint32_t K, float scale, uint32_t flags, int32_t* topk_ids, float* topk_w, void* stream);
+/*
+ * The same within the best groups of experts.  Expert e belongs to group e / (E / groups); `groups` divides E, at most 64.
+ * A group's score is the largest of what its experts are chosen by, or with FLUXMOE_ROUTE_GROUP_TOP2 (sigmoid scores
+ * only) the sum of the two largest, of one where a second is missing.  The top_groups groups with the largest scores,
+ * equal ones by ascending group, are kept, and the K experts are chosen among theirs: K <= top_groups * E / groups.
+ * A group none of whose experts can be chosen is not kept.  Gates that are not renormalised are of the softmax over all E.
+ * The gradient is fluxmoe_route_grad, as without groups.
+ */
+#define FLUXMOE_ROUTE_GROUP_TOP2 4u
+int fluxmoe_route_grouped(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride,
+                          const float* bias, uint32_t K, uint32_t groups, uint32_t top_groups, float scale,
+                          uint32_t flags, int32_t* topk_ids, float* topk_w, void* stream);
 /* Its gradient: d_logits (`type` [T][E], d_row_stride apart, written whole) from d_topk_w (device float [T][K]).
  * topk_ids as fluxmoe_route gave them (distinct in a row; others than 0..E-1 count as empty); which experts
  * are chosen, and the bias, have no gradient. */
@@ -546,6 +558,61 @@ int fluxmoe_block_norm_grad(const fluxmoe_norm_desc* desc, uint32_t T, const voi
                             const float* gate, const void* w_post, const void* w_pre, const void* d_residual_out,
                             const uint16_t* d_normed, void* d_residual, void* d_y, float* d_gate, float* d_w_post,
                             float* d_w_pre, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Experts in 4-bit floating point: weights kept in the microscaling format MXFP4, a quarter of BF16's bytes, for
+ * products on the rows that fluxmoe_sort_tokens and fluxmoe_dispatch put in order, with the gradients that training
+ * beside frozen experts takes.  As above: device pointers, no context, nothing kept or allocated, only enqueued; the same
+ * call gives the same bits.
+ *
+ * A row of MXFP4 is a row of codes, two columns to a byte (the even one in bits 0..3), and a row of scales, one byte
+ * for each 32 columns.  A code is a sign (bit 3) and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6; scale s stands for
+ * 2^(s - 127), 255 for not-a-number.  Columns are a multiple of 32, at most 2^20.
+ * ------------------------------------------------------------------------------------------ */
+#define FLUXMOE_MXFP4 2u
+
+/* x (`type` [rows][columns], x_stride elements apart) to codes and scales (strides in bytes).  With m the largest
+ * magnitude of 32 columns their scale is 2^(floor(log2 m) - 2), at least 2^-127; each x / scale goes to the nearest
+ * code, ties to the even one, and above 6 to 6.  A block with an infinity or a NaN gets scale 255 and codes 0. */
+int fluxmoe_mx_quantize(const void* x, uint32_t type, uint64_t rows, uint32_t columns, uint64_t x_stride, uint8_t* codes,
+                        uint64_t codes_stride, uint8_t* scales, uint64_t scales_stride, void* stream);
+/* And back: exact, but for numbers past the type's range (scales above 252), which become infinite. */
+int fluxmoe_mx_dequantize(const uint8_t* codes, uint64_t codes_stride, const uint8_t* scales, uint64_t scales_stride,
+                          uint64_t rows, uint32_t columns, void* out, uint32_t type, uint64_t out_stride, void* stream);
+
+/*
+ * Products by expert: out[r] = W_e rows[r] for the counts[e] rows from offsets[e] on (device int32 [E + 1] and [E], as
+ * fluxmoe_sort_tokens gives them; groups do not overlap).  Other rows of out are left as they were, and what of a group lies
+ * outside 0..rows_cap-1 is not done.
+ *   w_codes  device [E][N][K / 2], 16-byte aligned; w_scales device [E][N][K / 32]: N outputs by K columns to each
+ *            expert; E <= 4096, N <= 2^20
+ *   rows     rows_type FLUXMOE_BF16 [rows_cap][K], or FLUXMOE_MXFP4: codes with row_scales [rows_cap][K / 32]
+ *   out      out_type FLUXMOE_BF16 or FLUXMOE_F32 [rows_cap][N], not overlapping the rows; sums are FP32 and rounded once
+ * Strides are in elements (codes and scales: bytes) from one row to the next; 0: the row's width.  Rows at 16-byte
+ * addresses are read 16 bytes at a time, any others an element at a time.
+ */
+typedef struct {
+    uint32_t E, N, K;
+    uint32_t rows_type, out_type;
+    uint32_t reserved;                 /* 0 */
+    uint64_t rows_cap;
+    uint64_t rows_stride, row_scales_stride, out_stride;
+} fluxmoe_mx_product_desc;
+int fluxmoe_mx_product(const fluxmoe_mx_product_desc* desc, const void* rows, const uint8_t* row_scales, const int32_t* offsets,
+                       const int32_t* counts, const uint8_t* w_codes, const uint8_t* w_scales, void* out, void* stream);
+/* Its gradient to the rows, W_e being frozen: d_rows[r] = transpose(W_e) d_out[r], rows as above.  out_* describe d_out
+ * (BF16), rows_* d_rows (BF16 or FP32).  Rows in 4 bits have that of the rows they were made of. */
+int fluxmoe_mx_product_grad(const fluxmoe_mx_product_desc* desc, const uint16_t* d_out, const int32_t* offsets,
+                            const int32_t* counts, const uint8_t* w_codes, const uint8_t* w_scales, void* d_rows, void* stream);
+
+/* Between an expert's products: h[r][f] = g / (1 + e^-g) * u with g = gate_up[r][f], u = gate_up[r][ffn + f] (`type`
+ * [rows][2 ffn], h h_type [rows][ffn]; strides in elements).  And its gradient: d_gate_up, of gate_up's type, from d_h, of
+ * h's; it may be gate_up's own rows (then with their stride).  Rows that belong to no expert are passed through like the others. */
+int fluxmoe_swiglu(const void* gate_up, uint32_t type, uint64_t rows, uint32_t ffn, uint64_t gate_up_stride, void* h,
+                   uint32_t h_type, uint64_t h_stride, void* stream);
+int fluxmoe_swiglu_grad(const void* gate_up, uint32_t type, uint64_t rows, uint32_t ffn, uint64_t gate_up_stride,
+                        const void* d_h, uint32_t h_type, uint64_t d_h_stride, void* d_gate_up, uint64_t d_gate_up_stride,
+                        void* stream);
 
 /* Synchronous: read and clear the device error word (0 = none; bit 0 a block failed
  * validation during decode and was skipped, bit 1 an unmapped expert was routed to). */

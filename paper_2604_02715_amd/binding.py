@@ -66,6 +66,11 @@ class PagedTensorInfo(C.Structure):
                 ("pad_bytes", C.c_uint64), ("n_uncompressed", C.c_uint32), ("n_pageable", C.c_uint32)]
 
 
+class MxProductDesc(C.Structure):
+    _fields_ = ([(n, C.c_uint32) for n in ("E", "N", "K", "rows_type", "out_type", "reserved")]
+                + [(n, C.c_uint64) for n in ("rows_cap", "rows_stride", "row_scales_stride", "out_stride")])
+
+
 class NormDesc(C.Structure):
     _fields_ = ([(n, C.c_uint32) for n in ("hidden", "y_type", "residual_type", "weight_type", "flags")]
                 + [("eps", C.c_float), ("scale", C.c_float), ("reserved", C.c_uint32)]
@@ -74,8 +79,8 @@ class NormDesc(C.Structure):
                                              "d_normed_stride")])
 
 
-BF16, F32 = 0, 1
-ROUTE_SIGMOID, ROUTE_RENORMALIZE = 1, 2
+BF16, F32, MXFP4 = 0, 1, 2
+ROUTE_SIGMOID, ROUTE_RENORMALIZE, ROUTE_GROUP_TOP2 = 1, 2, 4
 NORM_GATE_TOKEN, NORM_GATE_CHANNEL, NORM_GATE_SIGMOID, NORM_ZERO_CENTRED = 1, 2, 4, 8
 
 PLAN_KEEP, PLAN_RECLAIM, PLAN_RESTORE, PLAN_SKIP, PLAN_DONE = 0, 1, -1, 2, 3
@@ -121,6 +126,8 @@ EXPORTS = {
     "fluxmoe_route_grad": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint64, C.c_void_p,
                                      C.c_uint32, C.c_float, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint64,
                                      C.c_void_p]),
+    "fluxmoe_route_grouped": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint32,
+                                        C.c_uint32, C.c_uint32, C.c_float, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p]),
     "fluxmoe_sorted_rows": (C.c_uint64, [C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32]),
     "fluxmoe_sort_workspace_bytes": (C.c_uint64, [C.c_uint32, C.c_uint32, C.c_uint32]),
     "fluxmoe_sort_tokens": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p,
@@ -138,6 +145,16 @@ EXPORTS = {
     "fluxmoe_block_norm_grad_workspace_bytes": (C.c_uint64, [C.c_uint32, C.c_uint32]),
     "fluxmoe_block_norm_grad": (C.c_int, [C.POINTER(NormDesc), C.c_uint32] + [C.c_void_p] * 13
                                 + [C.c_uint64, C.c_void_p]),
+    "fluxmoe_mx_quantize": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint64,
+                                      C.c_void_p, C.c_uint64, C.c_void_p]),
+    "fluxmoe_mx_dequantize": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint32, C.c_void_p,
+                                        C.c_uint32, C.c_uint64, C.c_void_p]),
+    "fluxmoe_mx_product": (C.c_int, [C.POINTER(MxProductDesc)] + [C.c_void_p] * 8),
+    "fluxmoe_mx_product_grad": (C.c_int, [C.POINTER(MxProductDesc)] + [C.c_void_p] * 7),
+    "fluxmoe_swiglu": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint32,
+                                 C.c_uint64, C.c_void_p]),
+    "fluxmoe_swiglu_grad": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint64, C.c_void_p, C.c_uint32,
+                                      C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]),
     "fluxmoe_stream_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p]),
     "fluxmoe_stream_mix": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_uint32, C.c_uint32,
                                      C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64), C.c_void_p]),
@@ -333,6 +350,12 @@ def fluxmoe_route_grad(logits_ptr, type_, T, E, row_stride, topk_ids_ptr, K, sca
                                     d_logits_ptr, d_row_stride, stream))
 
 
+def fluxmoe_route_grouped(logits_ptr, type_, T, E, row_stride, bias_ptr, K, groups, top_groups, scale, flags, topk_ids_ptr,
+                          topk_w_ptr, stream=None):
+    _check(lib().fluxmoe_route_grouped(logits_ptr, type_, T, E, row_stride, bias_ptr, K, groups, top_groups, scale, flags,
+                                       topk_ids_ptr, topk_w_ptr, stream))
+
+
 def fluxmoe_sorted_rows(T, K, E, align=1) -> int:
     return int(lib().fluxmoe_sorted_rows(T, K, E, align))
 
@@ -383,6 +406,37 @@ def fluxmoe_block_norm_grad(desc, T, y_ptr, residual_out_ptr, gate_ptr, w_post_p
     _check(lib().fluxmoe_block_norm_grad(desc, T, y_ptr, residual_out_ptr, gate_ptr, w_post_ptr, w_pre_ptr,
                                          d_residual_out_ptr, d_normed_ptr, d_residual_ptr, d_y_ptr, d_gate_ptr,
                                          d_w_post_ptr, d_w_pre_ptr, workspace_ptr, workspace_bytes, stream))
+
+
+# ---------------------------------------------------------------------- experts in 4-bit floating point
+def fluxmoe_mx_quantize(x_ptr, type_, rows, columns, x_stride, codes_ptr, codes_stride, scales_ptr, scales_stride, stream=None):
+    _check(lib().fluxmoe_mx_quantize(x_ptr, type_, rows, columns, x_stride, codes_ptr, codes_stride, scales_ptr, scales_stride,
+                                     stream))
+
+
+def fluxmoe_mx_dequantize(codes_ptr, codes_stride, scales_ptr, scales_stride, rows, columns, out_ptr, type_, out_stride,
+                          stream=None):
+    _check(lib().fluxmoe_mx_dequantize(codes_ptr, codes_stride, scales_ptr, scales_stride, rows, columns, out_ptr, type_,
+                                       out_stride, stream))
+
+
+def fluxmoe_mx_product(desc, rows_ptr, row_scales_ptr, offsets_ptr, counts_ptr, w_codes_ptr, w_scales_ptr, out_ptr, stream=None):
+    _check(lib().fluxmoe_mx_product(desc, rows_ptr, row_scales_ptr, offsets_ptr, counts_ptr, w_codes_ptr, w_scales_ptr, out_ptr,
+                                    stream))
+
+
+def fluxmoe_mx_product_grad(desc, d_out_ptr, offsets_ptr, counts_ptr, w_codes_ptr, w_scales_ptr, d_rows_ptr, stream=None):
+    _check(lib().fluxmoe_mx_product_grad(desc, d_out_ptr, offsets_ptr, counts_ptr, w_codes_ptr, w_scales_ptr, d_rows_ptr, stream))
+
+
+def fluxmoe_swiglu(gate_up_ptr, type_, rows, ffn, gate_up_stride, h_ptr, h_type, h_stride, stream=None):
+    _check(lib().fluxmoe_swiglu(gate_up_ptr, type_, rows, ffn, gate_up_stride, h_ptr, h_type, h_stride, stream))
+
+
+def fluxmoe_swiglu_grad(gate_up_ptr, type_, rows, ffn, gate_up_stride, d_h_ptr, h_type, d_h_stride, d_gate_up_ptr,
+                        d_gate_up_stride, stream=None):
+    _check(lib().fluxmoe_swiglu_grad(gate_up_ptr, type_, rows, ffn, gate_up_stride, d_h_ptr, h_type, d_h_stride, d_gate_up_ptr,
+                                     d_gate_up_stride, stream))
 
 
 def fluxmoe_stream_copy(dst_ptr, src_ptr, nbytes, n_workgroups, stream=None):

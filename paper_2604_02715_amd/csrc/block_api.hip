@@ -1,7 +1,7 @@
 // C entry points of the operators around the routed experts: argument checks, then one launcher call.  No context: they take
 // device pointers and sizes, keep nothing between calls and allocate nothing.
+#include "api_checks.h"
 #include "block_ops.h"
-#include "fluxmoe_internal.h"
 
 using namespace fluxmoe;
 
@@ -10,21 +10,11 @@ namespace {
 constexpr uint32_t kMaxTokens = 1u << 20;    // keeps every launch below 2^32 threads
 constexpr uint32_t kMaxHidden = 1u << 20;
 
-uint32_t elem_bytes(uint32_t type) { return type == FLUXMOE_F32 ? 4 : 2; }
-bool known(uint32_t type) { return type == FLUXMOE_BF16 || type == FLUXMOE_F32; }
-bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-// Rows of `bytes` per element, `stride` elements apart, each at a 16-byte address; absent tensors do not stand in the way.
-bool rows_aligned(const void* p, uint64_t stride, uint32_t bytes) { return !p || (aligned(p, 16) && stride * bytes % 16 == 0); }
-
 int check_tokens(uint32_t T) {
     return T <= kMaxTokens ? FLUXMOE_OK : set_error(FLUXMOE_EINVAL, "T must be at most %u (got %u)", kMaxTokens, T);
 }
 int check_hidden(uint32_t H) {
     return H >= 1 && H <= kMaxHidden ? FLUXMOE_OK : set_error(FLUXMOE_EINVAL, "hidden must be in 1..%u (got %u)", kMaxHidden, H);
-}
-int check_stride(const char* name, uint64_t stride, uint32_t width) {
-    if (stride >= width && stride < (1ull << 40)) return FLUXMOE_OK;
-    return set_error(FLUXMOE_EINVAL, "%s (%llu) must be at least the row's %u elements", name, (unsigned long long)stride, width);
 }
 int check_experts(uint32_t E, uint32_t K) {
     if (E == 0 || E > kRouteMaxExperts) return set_error(FLUXMOE_EINVAL, "E must be in 1..%u (got %u)", kRouteMaxExperts, E);
@@ -38,6 +28,35 @@ int check_route(uint32_t type, uint32_t T, uint32_t E, uint32_t K, uint32_t flag
     if (int rc = check_experts(E, K)) return rc;
     if (!known(type)) return set_error(FLUXMOE_EINVAL, "unknown element type %u", type);
     if (flags & ~(FLUXMOE_ROUTE_SIGMOID | FLUXMOE_ROUTE_RENORMALIZE)) return set_error(FLUXMOE_EINVAL, "unknown flags 0x%x", flags);
+    return FLUXMOE_OK;
+}
+
+// Both forms of the router, behind the checks that are their own.
+int route(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride, const float* bias, uint32_t K, uint32_t groups,
+          uint32_t top_groups, float scale, uint32_t flags, int32_t* topk_ids, float* topk_w, void* stream) {
+    if (bias && !(flags & FLUXMOE_ROUTE_SIGMOID)) return set_error(FLUXMOE_EINVAL, "bias goes with FLUXMOE_ROUTE_SIGMOID");
+    if (T == 0) return FLUXMOE_OK;
+    if (!logits || !topk_ids || !topk_w) return set_error(FLUXMOE_EINVAL, "NULL argument");
+    if (int rc = check_stride("row_stride", row_stride, E)) return rc;
+    const uint32_t bytes = elem_bytes(type);
+    if (!aligned(logits, bytes) || !aligned(bias, 4) || !aligned(topk_ids, 4) || !aligned(topk_w, 4))
+        return set_error(FLUXMOE_EINVAL, "a pointer is not aligned to its elements");
+    RouteArgs a{};
+    a.logits = logits;
+    a.bias = bias;
+    a.ids = topk_ids;
+    a.gates = topk_w;
+    a.row_stride = row_stride;
+    a.T = T;
+    a.E = E;
+    a.K = K;
+    a.scale = scale;
+    a.groups = groups;
+    a.top_groups = top_groups;
+    a.group_top2 = (flags & FLUXMOE_ROUTE_GROUP_TOP2) != 0;
+    a.renormalize = (flags & FLUXMOE_ROUTE_RENORMALIZE) != 0;
+    a.vec = rows_aligned(logits, row_stride, bytes);
+    HIPCHECK(launch_route(a, type == FLUXMOE_F32, (flags & FLUXMOE_ROUTE_SIGMOID) != 0, static_cast<hipStream_t>(stream)));
     return FLUXMOE_OK;
 }
 
@@ -107,27 +126,19 @@ extern "C" {
 int fluxmoe_route(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride, const float* bias, uint32_t K, float scale,
                   uint32_t flags, int32_t* topk_ids, float* topk_w, void* stream) {
     if (int rc = check_route(type, T, E, K, flags)) return rc;
-    if (bias && !(flags & FLUXMOE_ROUTE_SIGMOID)) return set_error(FLUXMOE_EINVAL, "bias goes with FLUXMOE_ROUTE_SIGMOID");
-    if (T == 0) return FLUXMOE_OK;
-    if (!logits || !topk_ids || !topk_w) return set_error(FLUXMOE_EINVAL, "NULL argument");
-    if (int rc = check_stride("row_stride", row_stride, E)) return rc;
-    const uint32_t bytes = elem_bytes(type);
-    if (!aligned(logits, bytes) || !aligned(bias, 4) || !aligned(topk_ids, 4) || !aligned(topk_w, 4))
-        return set_error(FLUXMOE_EINVAL, "a pointer is not aligned to its elements");
-    RouteArgs a{};
-    a.logits = logits;
-    a.bias = bias;
-    a.ids = topk_ids;
-    a.gates = topk_w;
-    a.row_stride = row_stride;
-    a.T = T;
-    a.E = E;
-    a.K = K;
-    a.scale = scale;
-    a.renormalize = (flags & FLUXMOE_ROUTE_RENORMALIZE) != 0;
-    a.vec = rows_aligned(logits, row_stride, bytes);
-    HIPCHECK(launch_route(a, type == FLUXMOE_F32, (flags & FLUXMOE_ROUTE_SIGMOID) != 0, static_cast<hipStream_t>(stream)));
-    return FLUXMOE_OK;
+    return route(logits, type, T, E, row_stride, bias, K, 1, 1, scale, flags, topk_ids, topk_w, stream);
+}
+
+int fluxmoe_route_grouped(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride, const float* bias, uint32_t K,
+                          uint32_t groups, uint32_t top_groups, float scale, uint32_t flags, int32_t* topk_ids, float* topk_w, void* stream) {
+    if (int rc = check_route(type, T, E, K, flags & ~FLUXMOE_ROUTE_GROUP_TOP2)) return rc;
+    if (groups == 0 || groups > kRouteMaxGroups || E % groups)
+        return set_error(FLUXMOE_EINVAL, "groups must be in 1..%u and divide E (got %u of %u)", kRouteMaxGroups, groups, E);
+    if (top_groups == 0 || top_groups > groups) return set_error(FLUXMOE_EINVAL, "top_groups must be in 1..groups (got %u of %u)", top_groups, groups);
+    if (K > top_groups * (E / groups)) return set_error(FLUXMOE_EINVAL, "K (%u) exceeds the experts of %u groups", K, top_groups);
+    if ((flags & FLUXMOE_ROUTE_GROUP_TOP2) && !(flags & FLUXMOE_ROUTE_SIGMOID))
+        return set_error(FLUXMOE_EINVAL, "FLUXMOE_ROUTE_GROUP_TOP2 goes with FLUXMOE_ROUTE_SIGMOID");
+    return route(logits, type, T, E, row_stride, bias, K, groups, top_groups, scale, flags, topk_ids, topk_w, stream);
 }
 
 int fluxmoe_route_grad(const void* logits, uint32_t type, uint32_t T, uint32_t E, uint64_t row_stride, const int32_t* topk_ids, uint32_t K,

@@ -10,6 +10,7 @@ namespace fluxmoe {
 // ---------------------------------------------------------------- router (route_kernels.hip)
 constexpr uint32_t kRouteMaxExperts = 4096;
 constexpr uint32_t kRouteMaxTopK = 64;       // a lane of the wavefront keeps a chosen expert
+constexpr uint32_t kRouteMaxGroups = 64;     // and one, or several, look through a group
 
 struct RouteArgs {
     const void* logits;          // [T][E], rows row_stride elements apart
@@ -21,6 +22,8 @@ struct RouteArgs {
     uint64_t row_stride, d_stride;
     uint32_t T, E, K;
     uint32_t renormalize;
+    uint32_t groups, top_groups; // 1, 1: none
+    uint32_t group_top2;         // a group's score: the sum of its two best keys, otherwise its best
     uint32_t vec, d_vec;         // rows are 16-byte aligned
     float scale;
 };

@@ -93,8 +93,58 @@ __device__ __forceinline__ void lane_best(const uint32_t (&key)[NV], uint32_t& b
         if (key[j] > best) { best = key[j]; at = j; }
 }
 
-template <typename L, int LPR, int NV, bool SIGMOID>
+// Takes the experts of the groups that are not kept out of a row's keys.  Each of a row's groups belongs to as many lanes as there are
+// for it (a power of two); they share its keys out, and the two largest of each part meet in the steps of a reduction.  A group is kept
+// if fewer than top_groups groups come before it, which every lane counts for its own.  s_row: the row's keys, one word apart after
+// each group so that lanes of different groups read different banks; s_group: its groups' scores.
+template <int LPR, int NV>
+__device__ __forceinline__ void keep_groups(const RouteArgs& a, uint32_t sub, uint32_t (&key)[NV], uint32_t* s_row, uint32_t* s_group) {
+    const uint32_t size = a.E / a.groups, first = sub * NV;
+    uint32_t g = first / size, at = first - g * size;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (first + j < a.E) s_row[first + j + g] = key[j];
+        if (++at == size) { at = 0; ++g; }
+    }
+    wave_fence();
+    uint32_t lanes = LPR;                                // to a group
+    while (lanes * a.groups > LPR) lanes /= 2;
+    const uint32_t group = sub / lanes;
+    uint32_t one = 0, two = 0;
+    if (group < a.groups)
+        for (uint32_t i = sub & (lanes - 1); i < size; i += lanes) {
+            const uint32_t k = s_row[group * (size + 1) + i];
+            two = max(two, min(one, k));
+            one = max(one, k);
+        }
+    for (uint32_t d = 1; d < lanes; d *= 2) {
+        const uint32_t o = __shfl_xor(one, d), t = __shfl_xor(two, d);
+        two = max(max(two, t), min(one, o));
+        one = max(one, o);
+    }
+    // the sum is rounded as written; a score that sank to minus infinity is still one
+    const uint32_t score = a.group_top2 && two ? max(order_key(key_value(one) + key_value(two)), 1u) : one;
+    if (group < a.groups && (sub & (lanes - 1)) == 0) s_group[group] = score;
+    wave_fence();
+    uint32_t ahead = 0;
+    for (uint32_t o = 0; o < a.groups; ++o) {
+        const uint32_t k = s_group[o];
+        ahead += k > score || (k == score && o < group);
+    }
+    const uint64_t kept = __ballot(group < a.groups && score != 0 && ahead < a.top_groups) >> (threadIdx.x & 63 & ~(LPR - 1));
+    g = first / size;
+    at = first - g * size;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (g >= a.groups || !((kept >> (g * lanes)) & 1)) key[j] = 0;
+        if (++at == size) { at = 0; ++g; }
+    }
+}
+
+template <typename L, int LPR, int NV, bool SIGMOID, bool GROUPED>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+    __shared__ uint32_t s_keys[GROUPED ? kThreads / LPR : 1][GROUPED ? LPR * NV + kRouteMaxGroups : 1];
+    __shared__ uint32_t s_groups[GROUPED ? kThreads / LPR : 1][GROUPED ? kRouteMaxGroups : 1];
     __shared__ int32_t s_id[kThreads];           // a row's K results lie at its first lane's number and behind it (K <= LPR)
     __shared__ uint32_t s_key[kThreads];
     const uint32_t tid = threadIdx.x, sub = tid & (LPR - 1), base = tid - sub;
@@ -114,12 +164,23 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     s_key[tid] = 0;
     wave_fence();
 
-    uint32_t best, at;
+    uint32_t best, at, top_key = 0;
     lane_best<NV>(key, best, at);
     float total = 0.0f;
+    if constexpr (GROUPED) {
+        if (!SIGMOID && !a.renormalize) {                // the whole row's softmax, whichever groups are kept
+            top_key = group_max<LPR>(best);
+            const float top = key_value(top_key);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) total += key[j] ? softmax_term(key_value(key[j]), top) : 0.0f;
+            total = group_sum<LPR>(total);
+        }
+        keep_groups<LPR, NV>(a, sub, key, s_keys[tid / LPR], s_groups[tid / LPR]);
+        lane_best<NV>(key, best, at);
+    }
     for (uint32_t k = 0; k < a.K; ++k) {
         const uint32_t most = group_max<LPR>(best);
-        if (!SIGMOID && k == 0 && !a.renormalize) {      // the whole row's softmax
+        if (!GROUPED && !SIGMOID && k == 0 && !a.renormalize) {      // the whole row's softmax
             const float top = key_value(most);
 #pragma unroll
             for (int j = 0; j < NV; ++j) total += key[j] ? softmax_term(key_value(key[j]), top) : 0.0f;
@@ -142,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     float p = 0.0f;
     if (chosen) {
         if constexpr (SIGMOID) p = sigmoid(to_float(logits[id]));
-        else p = softmax_term(key_value(s_key[tid]), key_value(s_key[base]));
+        else p = softmax_term(key_value(s_key[tid]), key_value(GROUPED && !a.renormalize ? top_key : s_key[base]));
     }
     if (a.renormalize) {
         total = group_sum<LPR>(p);
@@ -348,9 +409,9 @@ uint32_t workgroups(const RouteArgs& a, uint32_t lanes) {
     const uint32_t rows = kThreads / lanes;
     return (a.T + rows - 1) / rows;
 }
-template <typename L, bool SIGMOID, int LPR, int NV>
+template <typename L, bool SIGMOID, int LPR, int NV, bool GROUPED = false>
 void go(const RouteArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((route_kernel<L, LPR, NV, SIGMOID>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((route_kernel<L, LPR, NV, SIGMOID, GROUPED>), dim3(workgroups(a, LPR)), dim3(kThreads), 0, stream, a);
 }
 template <typename L, bool SIGMOID, int LPR, int CHUNKS>
 void go_many(const RouteArgs& a, hipStream_t stream) {
@@ -378,6 +439,17 @@ void go_grad(const RouteArgs& a, hipStream_t stream) {
 //   256, 2   1.42         1.27         1.28         1.14         1.22         0.99
 // Up to 128 experts and from 257 on they are level about 4096 rows.
 uint32_t many_rows(uint32_t E) { return E <= 128 || E > 256 ? 4096 : E <= 192 ? 6144 : 8192; }
+
+// The same with a lane for every group, too.
+template <typename L, bool SIGMOID>
+void pick_grouped(const RouteArgs& a, hipStream_t stream) {
+    if (a.E <= 64 && a.K <= 8 && a.groups <= 8) go<L, SIGMOID, 8, 8, true>(a, stream);
+    else if (a.E <= 256 && a.K <= 32 && a.groups <= 32) go<L, SIGMOID, 32, 8, true>(a, stream);
+    else if (a.E <= 512) go<L, SIGMOID, 64, 8, true>(a, stream);
+    else if (a.E <= 1024) go<L, SIGMOID, 64, 16, true>(a, stream);
+    else if (a.E <= 2048) go<L, SIGMOID, 64, 32, true>(a, stream);
+    else go<L, SIGMOID, 64, 64, true>(a, stream);
+}
 
 // As few lanes to a row as hold its experts at eight each, and one for every chosen expert.
 template <typename L, bool SIGMOID>
@@ -412,6 +484,7 @@ void pick_grad(const RouteArgs& a, hipStream_t stream) {
 template <typename L, bool SIGMOID>
 hipError_t pick(const RouteArgs& a, bool grad, hipStream_t stream) {
     if (grad) pick_grad<L, SIGMOID>(a, stream);
+    else if (a.groups > 1) pick_grouped<L, SIGMOID>(a, stream);
     else pick<L, SIGMOID>(a, stream);
     return hipGetLastError();
 }

@@ -91,8 +91,13 @@ def _logits(logits):
     return device, T, E, _matrix(logits, "logits", T, E, device)
 
 
-def route(logits, ids, gates, *, bias=None, scale=1.0, score="softmax", renormalize=True, stream=None):
-    """ids (int32), gates (float32) [T][K] <- logits [T][E]; bias float32 [E], sigmoid scores only."""
+def route(logits, ids, gates, *, bias=None, scale=1.0, score="softmax", renormalize=True, groups=1, top_groups=1, group_score="max",
+          stream=None):
+    """ids (int32), gates (float32) [T][K] <- logits [T][E]; bias float32 [E], sigmoid scores only.  With `groups` neighbouring groups of
+    E / groups experts each, the experts are chosen among those of the top_groups best ones, by their best expert ("max") or the sum of
+    their two best ("top2", sigmoid scores only)."""
+    if group_score not in ("max", "top2"):
+        _fail("group_score must be 'max' or 'top2', got %r" % (group_score,))
     device, T, E, stride = _logits(logits)
     if ids.dim() != 2:
         _fail("ids must be [tokens][top_k]")
@@ -103,8 +108,16 @@ def route(logits, ids, gates, *, bias=None, scale=1.0, score="softmax", renormal
     _whole(gates, "gates", (T, K), torch.float32, device)
     if bias is not None:
         _whole(bias, "bias", (E,), torch.float32, device)
-    B.fluxmoe_route(logits.data_ptr(), _TYPES[logits.dtype], T, E, stride, _ptr(bias), K, scale, _route_flags(score, renormalize),
-                    ids.data_ptr(), gates.data_ptr(), _sptr(stream, device))
+    flags = _route_flags(score, renormalize)
+    if groups == 1 and top_groups == 1 and group_score == "max":
+        B.fluxmoe_route(logits.data_ptr(), _TYPES[logits.dtype], T, E, stride, _ptr(bias), K, scale, flags, ids.data_ptr(), gates.data_ptr(),
+                        _sptr(stream, device))
+        return
+    if (groups | top_groups) >> 32:
+        _too_large()
+    B.fluxmoe_route_grouped(logits.data_ptr(), _TYPES[logits.dtype], T, E, stride, _ptr(bias), K, groups, top_groups, scale,
+                            flags | (B.ROUTE_GROUP_TOP2 if group_score == "top2" else 0), ids.data_ptr(), gates.data_ptr(),
+                            _sptr(stream, device))
 
 
 def route_grad(logits, ids, d_gates, d_logits, *, scale=1.0, score="softmax", renormalize=True, stream=None):
