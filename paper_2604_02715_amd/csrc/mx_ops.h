@@ -51,6 +51,9 @@ struct MxProductArgs {
     uint32_t out_vec;            // out's rows at 16-byte addresses
 };
 hipError_t launch_mx_product(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream);
+// 256 x 256 tiles (mx_tiles.hip)
+bool mx_wide_takes(const MxProductArgs& a, bool mx_rows);
+hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream);
 hipError_t launch_mx_product_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream);
 
 }  // namespace fluxmoe

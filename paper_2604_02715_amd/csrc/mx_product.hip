@@ -7,85 +7,13 @@
 // rows in the BF16 matrix instructions; rows in 4 bits themselves go to the scaled ones as they are.  Sums are FP32.
 //
 // Which rows are whose is known on the device only: a workgroup adds up the experts' tiles and finds its own (find_tile).
-#include "block_device.h"
-#include "mx_ops.h"
+#include "mx_device.h"
 
 namespace fluxmoe {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kMaxGrid = 1u << 22;
-
-struct Tile {
-    uint32_t expert, first, rows;            // rows 0: no such tile
-};
-
-// Rows of expert e that lie within the matrix, whatever offsets and counts hold.
-__device__ __forceinline__ uint32_t rows_of(const MxProductArgs& a, uint32_t e) {
-    const int32_t c = a.counts[e], o = a.offsets[e];
-    if (c <= 0 || o < 0 || uint32_t(o) >= a.cap) return 0;
-    return min(uint32_t(c), a.cap - uint32_t(o));
-}
-
-// Tile number `wanted` of the experts' groups in their order, `size` rows to a tile.  All threads of the workgroup; a thread
-// adds up neighbouring experts.  s: kThreads / 64 + 4 words of LDS.
-__device__ __forceinline__ Tile find_tile(const MxProductArgs& a, uint32_t size, uint32_t wanted, uint32_t* s) {
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t per = (a.E + kThreads - 1) / kThreads, from = min(tid * per, a.E), to = min(from + per, a.E);
-    uint32_t mine = 0;
-    for (uint32_t e = from; e < to; ++e) mine += (rows_of(a, e) + size - 1) / size;
-    uint32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const uint32_t below = __shfl_up(upto, d);
-        if (lane >= uint32_t(d)) upto += below;
-    }
-    __syncthreads();                                     // the last tile's readers are done with s
-    if (lane == 63) s[wave] = upto;
-    if (tid == 0) s[kThreads / 64 + 2] = 0;
-    __syncthreads();
-    for (uint32_t w = 0; w < wave; ++w) upto += s[w];
-    uint32_t before = upto - mine;
-    if (wanted >= before && wanted < upto) {
-        for (uint32_t e = from; e < to; ++e) {
-            const uint32_t rows = rows_of(a, e), tiles = (rows + size - 1) / size;
-            if (wanted < before + tiles) {
-                const uint32_t at = (wanted - before) * size;
-                s[kThreads / 64] = e;
-                s[kThreads / 64 + 1] = uint32_t(a.offsets[e]) + at;
-                s[kThreads / 64 + 2] = min(size, rows - at);
-                break;
-            }
-            before += tiles;
-        }
-    }
-    __syncthreads();
-    Tile t;
-    t.expert = __builtin_amdgcn_readfirstlane(s[kThreads / 64]);
-    t.first = __builtin_amdgcn_readfirstlane(s[kThreads / 64 + 1]);
-    t.rows = __builtin_amdgcn_readfirstlane(s[kThreads / 64 + 2]);
-    return t;
-}
-
-// `records` bytes from `base` on, by offset: reads past them give 0
-__device__ __forceinline__ row_t bytes_at(const void* base, uint64_t offset, uint32_t records) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + offset), 0, int(records), 0x00020000);
-}
-constexpr uint32_t kNowhere = 0x7FFFFFF0u;               // an offset past any resource's records
-
-__device__ __forceinline__ float scale_operand(uint32_t s) { return __uint_as_float(s << 23); }
-
-// Eight codes as BF16
-__device__ __forceinline__ bf16x8 codes_bf16(uint32_t codes, float scale) {
-    const u32x4 v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
-    return __builtin_bit_cast(bf16x8, v);
-}
 
 // ---------------------------------------------------------------- few rows to an expert: bound by the weights' bytes
 // A workgroup has a tile of 16 MI rows and 16 NI outputs; its four wavefronts share out the columns, 128 at a time.  Lane
@@ -94,13 +22,13 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t codes, float scale) {
 // weights go from memory to registers to the matrix cores with nothing between; a row's columns are loaded likewise.
 template <int MI, int NI, bool MX, bool VEC, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
-    __shared__ uint32_t s_tile[kThreads / 64 + 4];
+    __shared__ uint32_t s_tile[kTileWords];
     __shared__ f32x4 s_acc[4][MI * NI][64];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4;
     const uint32_t blocks = a.K / kMxBlock, groups = (blocks + 3) / 4;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
-        const Tile t = find_tile(a, 16 * MI, tile_at, s_tile);
+        const Tile t = find_tile<kThreads>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;                         // nor are there any behind it
         const uint32_t n0 = strip * (16 * NI), outs = min(a.N - n0, uint32_t(16 * NI));
         const uint64_t w_row = uint64_t(t.expert) * a.N + n0;
@@ -197,14 +125,14 @@ __device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t piece) { ret
 template <bool GRAD, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_tile_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
     constexpr uint32_t BM = 128, BN = 128;
-    __shared__ uint32_t s_tile[kThreads / 64 + 4];
+    __shared__ uint32_t s_tile[kTileWords];
     __shared__ u32x4 s_x[BM * 8], s_w[BN * 8];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t sum = GRAD ? a.N : a.K, outs = GRAD ? a.K : a.N, blocks = a.K / kMxBlock;
     const uint32_t m_wave = (wave >> 1) * 64, n_wave = (wave & 1) * 64;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
-        const Tile t = find_tile(a, BM, tile_at, s_tile);
+        const Tile t = find_tile<kThreads>(a, BM, tile_at, s_tile);
         if (t.rows == 0) return;
         const uint32_t n0 = strip * BN;
         const char* x = static_cast<const char*>(a.rows) + uint64_t(t.first) * a.row_stride;
@@ -331,6 +259,7 @@ void go_tile(const MxProductArgs& a, hipStream_t stream) {
 template <typename OUT>
 hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
+    if (per_expert > 32 && mx_wide_takes(a, mx_rows)) return launch_mx_wide(a, mx_rows, sizeof(OUT) == 4, stream);
     if (mx_rows) {
         if (a.rows_vec) go_stream<2, 4, true, true, OUT>(a, stream);
         else go_stream<2, 4, true, false, OUT>(a, stream);

@@ -1,0 +1,401 @@
+// The product with experts' weights in 4-bit floating point where an expert has many rows: bound by the matrix cores.
+//
+// A workgroup's tile is 256 rows by 256 outputs, eight wavefronts as 4 (rows) x 2 (outputs), two to a SIMD, 64 x 128 each as
+// 2 x 4 tiles of the 32x32 matrix instructions.  Both operands go from memory straight to LDS, as they are: rows of 128 bytes, which are
+// 256 columns of codes (a superblock: eight blocks of 32, a 16-byte piece each) or 64 columns of BF16.  A load fills 1 KiB of LDS
+// without gaps, so instead of padding, the lane that fills position p of a row fetches piece p ^ ((row >> 1) & 7): 16 neighbouring
+// rows' pieces of one number then lie in 64 different banks.
+// Which columns a matrix instruction's k numbers stand for is free as long as both operands agree.  Lanes 0..31 take the first half
+// of a superblock's blocks and lanes 32..63 the second, so that a lane's scales of a superblock are four neighbouring bytes.
+#include "mx_device.h"
+
+namespace fluxmoe {
+namespace {
+
+constexpr uint32_t kTile = 256;
+constexpr int kStage = 32768;                            // 256 rows of 128 bytes
+constexpr uint32_t kThreads = 512;
+
+// Where a workgroup's tile lies.  Workgroups go to the eight XCDs in turn; the 32 that run on one at a time take a super-tile of
+// 32 >> sn_log2 row tiles by 1 << sn_log2 strips, whose rows and weights they share in that XCD's L2.
+struct WideGrid {
+    uint32_t strips, sn_log2, row_tiles, total;
+    __host__ WideGrid(uint64_t row_tiles_most, uint32_t outs) {
+        strips = (outs + kTile - 1) / kTile;
+        sn_log2 = 0;
+        while (sn_log2 < 3 && (1u << sn_log2) < strips) ++sn_log2;
+        row_tiles = uint32_t(row_tiles_most);
+        const uint64_t sm = 32u >> sn_log2, supers = (row_tiles_most + sm - 1) / sm * ((strips + (1u << sn_log2) - 1) >> sn_log2);
+        total = uint32_t((supers + 7) / 8 * 256);
+    }
+    __device__ __forceinline__ bool locate(uint32_t L, uint32_t& row_tile, uint32_t& strip) const {
+        const uint32_t sn = 1u << sn_log2, sm = 32u >> sn_log2, n_sn = (strips + sn - 1) >> sn_log2;
+        const uint32_t xcd = L % 8u, jj = L / 8u, st = jj / 32u * 8u + xcd, within = jj % 32u;
+        row_tile = st / n_sn * sm + (within >> sn_log2);
+        strip = st % n_sn * sn + (within & (sn - 1));
+        return strip < strips && row_tile < row_tiles;
+    }
+};
+
+// 16 bytes to each lane's place of the KiB at lds_addr, from its offset to the wavefront's base.  Assembly on purpose: with the compiler's builtin every later LDS read
+// waits for all loads into LDS that are under way, as it cannot tell that they fill another stage.  The waits are those written below, ahead of
+// the barriers.  M0 holds the destination; the compiler has reserved it, so its value is put back.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds_addr) {
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved) : "v"(offset), "s"(base), "s"(lds_addr) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
+// The four scales of blocks `at` .. `at` + 3 of a row of `blocks` that lies `row` bytes into m, 0 past its end.  WHOLE: they are whole words.
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t four_scales(row_t m, uint32_t row, uint32_t at, uint32_t blocks) {
+    if constexpr (WHOLE) return __builtin_amdgcn_raw_buffer_load_b32(m, at < blocks ? row + at : kNowhere, 0, kCached);
+    uint32_t v[4];
+#pragma unroll
+    for (uint32_t b = 0; b < 4; ++b) v[b] = __builtin_amdgcn_raw_buffer_load_b8(m, at + b < blocks ? row + at + b : kNowhere, 0, kCached);
+    return v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24;
+}
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+// WHOLE: scales are read four at a time
+template <bool MX, bool WHOLE, typename OUT>
+__global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, WideGrid grid) {
+    extern __shared__ __align__(16) uint8_t lds[];           // rows' two stages, weights' two stages, find_tile's words
+    uint32_t row_tile, strip;
+    if (!grid.locate(blockIdx.x, row_tile, strip)) return;
+    const Tile t = find_tile<kThreads>(a, kTile, row_tile, reinterpret_cast<uint32_t*>(lds + 4 * kStage));
+    if (t.rows == 0) return;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t wm = wave >> 1, wn = wave & 1, q = lane & 31, h = lane >> 5;
+    const uint32_t n0 = strip * kTile, blocks = a.K / kMxBlock, supers = (blocks + 7) / 8;
+    const uint32_t lds_base = uint32_t(uintptr_t((__attribute__((address_space(3))) void*)lds));
+
+    // What the lane fetches: four KiB of each operand to a wavefront and stage, rows 8 (4 wave + i) + lane / 8.
+    const uint8_t* const x_base = static_cast<const uint8_t*>(a.rows) + uint64_t(t.first) * a.row_stride;
+    const uint8_t* const w_base = a.w + (uint64_t(t.expert) * a.N + n0) * (a.K / 2);
+    uint32_t x_off[4], w_off[4];                             // of the rows
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t row = 8 * (wave * 4 + i) + (lane >> 3);
+        x_off[i] = min(row, t.rows - 1) * uint32_t(a.row_stride);
+        w_off[i] = min(row, a.N - 1 - n0) * (a.K / 2);
+    }
+    auto piece_of = [&](int i) __attribute__((always_inline)) { return (lane & 7) ^ ((4 * (i & 1) + (lane >> 4)) & 7); };
+    // Past the end of a row its last block is fetched in place of those that are missing, whose weights become 0 ahead of their products.
+    auto fetch_w = [&](int i, uint32_t super) __attribute__((always_inline)) {
+        load_to_lds(w_base + uint64_t(super) * 128, w_off[i] + min(piece_of(i), blocks - 1 - super * 8) * 16,
+                    lds_base + (2 + (super & 1)) * kStage + (wave * 4 + i) * 1024);
+    };
+    // the rows' codes of a superblock, or BF16 columns of its blocks s and 4 + s, into stage `to`
+    auto fetch_x = [&](int i, uint32_t super, uint32_t s, uint32_t to) __attribute__((always_inline)) {
+        const uint32_t block = min(MX ? piece_of(i) : s + 4 * (piece_of(i) >> 2), blocks - 1 - super * 8);
+        load_to_lds(x_base + uint64_t(super) * (MX ? 128 : 512), x_off[i] + block * (MX ? 16 : 64) + (MX ? 0 : (piece_of(i) & 3) * 16),
+                    lds_base + to * kStage + (wave * 4 + i) * 1024);
+    };
+
+    const row_t ws_at = bytes_at(a.ws, (uint64_t(t.expert) * a.N + n0) * blocks, min(kTile, a.N - n0) * blocks);
+    const row_t xs_at = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
+    auto w_scales = [&](int j, uint32_t super) __attribute__((always_inline)) {
+        return four_scales<WHOLE>(ws_at, min(wn * 128 + j * 32 + q, a.N - 1 - n0) * blocks, super * 8 + 4 * h, blocks);
+    };
+    auto x_scales = [&](int i, uint32_t super) __attribute__((always_inline)) {
+        return four_scales<WHOLE>(xs_at, min((wm + 4 * i) * 32 + q, t.rows - 1) * uint32_t(a.row_scales_stride), super * 8 + 4 * h, blocks);
+    };
+
+    f32x16 acc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    // Piece 4 h + ks of the lane's rows: the rows of a wavefront's 32 x 32 tiles lie 32 apart, which leaves the place of a piece as it is.
+    uint32_t at[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) at[ks] = q * 128 + 16 * ((4 * h + ks) ^ ((q >> 1) & 7));
+    auto read = [&](uint32_t addr) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(lds + addr); };
+    auto read_x = [&](int i, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + (stage * kStage + wm * 4096) + i * 16384); };
+    auto read_w = [&](int j, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + ((2 + stage) * kStage + wn * 16384) + j * 4096); };
+
+    // ACT: row groups wm, wm + 4 of the tile that have rows
+    auto k_loop = [&](auto ACT) __attribute__((always_inline)) {
+        constexpr int act = decltype(ACT)::value;
+        if constexpr (MX) {
+            // A step is a superblock, a sub-step 64 of its columns: blocks ks and 4 + ks.  Fragments of the next sub-step are read between
+            // the matrix instructions; a step's one barrier lies ahead of its last sub-step, which covers the first reads from the other stage.
+            uint32_t ws[4], xs[2], ws_next[4], xs_next[2];
+            u32x4 fx[2][2], fw[2][4];
+            auto fetch_scales = [&](uint32_t super) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) ws_next[j] = w_scales(j, super);
+#pragma unroll
+                for (int i = 0; i < act; ++i) xs_next[i] = x_scales(i, super);
+            };
+            auto scales_arrive = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { asm volatile("" : "+v"(ws_next[j])); }
+#pragma unroll
+                for (int i = 0; i < act; ++i) { asm volatile("" : "+v"(xs_next[i])); }
+            };
+            auto take_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) ws[j] = ws_next[j];
+#pragma unroll
+                for (int i = 0; i < act; ++i) xs[i] = xs_next[i];
+            };
+            auto read_item = [&](int n, uint32_t stage, int ks, int set) __attribute__((always_inline)) {
+                if (act == 0) return;
+                if (n < 4) fw[set][n] = read_w(n, ks, stage);
+                else if (n - 4 < act) fx[set][n - 4] = read_x(n - 4, ks, stage);
+            };
+            auto sub = [&](auto KS, auto NEXT, auto LOAD, uint32_t stage, uint32_t super) __attribute__((always_inline)) {
+                constexpr int ks = decltype(KS)::value, set = ks & 1;
+                constexpr bool next = decltype(NEXT)::value != 0, load = decltype(LOAD)::value != 0;
+                if constexpr (!next && act > 0) {           // 0 for blocks past the end; the rows' codes are finite whatever they are
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) fw[set][j][c] = super * 8 + 4 * h + ks < blocks ? fw[set][j][c] : 0;
+                }
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const int i = n / 4, j = n % 4;
+                    if (i < act) {
+                        const i32x8 xv = {int(fx[set][i][0]), int(fx[set][i][1]), int(fx[set][i][2]), int(fx[set][i][3]), 0, 0, 0, 0};
+                        const i32x8 wv = {int(fw[set][j][0]), int(fw[set][j][1]), int(fw[set][j][2]), int(fw[set][j][3]), 0, 0, 0, 0};
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xv, wv, acc[i][j], 4, 4, ks, int(xs[i]), ks, int(ws[j]));
+                    }
+                    if (ks < 3) {
+                        if (n < 6) read_item(n, stage, ks + 1, set ^ 1);
+                    } else {
+                        if (next && n < 6) read_item(n, stage ^ 1, 0, set ^ 1);
+                        if (load) {
+                            if (n & 1) fetch_w(n / 2, super + 2);
+                            else fetch_x(n / 2, super + 2, 0, stage);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            auto step = [&](auto NEXT, auto LOAD, uint32_t super) __attribute__((always_inline)) {
+                const uint32_t stage = super & 1;
+                if constexpr (decltype(NEXT)::value != 0) fetch_scales(super + 1);
+                sub(Int<0>{}, NEXT, LOAD, stage, super);
+                sub(Int<1>{}, NEXT, LOAD, stage, super);
+                sub(Int<2>{}, NEXT, LOAD, stage, super);
+                wait_loads<0>();
+                scales_arrive();
+                __syncthreads();
+                sub(Int<3>{}, NEXT, LOAD, stage, super);
+                take_scales();
+            };
+            fetch_scales(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { fetch_w(i, 0); fetch_x(i, 0, 0, 0); }
+            wait_loads<0>();
+            scales_arrive();
+            take_scales();
+            if (supers > 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { fetch_w(i, 1); fetch_x(i, 1, 0, 1); }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < 6; ++n) read_item(n, 0, 0, 0);
+            uint32_t super = 0;
+            for (; super + 2 < supers; ++super) step(Int<1>{}, Int<1>{}, super);
+            if (super + 1 < supers) step(Int<1>{}, Int<0>{}, super++);
+            step(Int<0>{}, Int<0>{}, super);
+        } else {
+            // A step is 64 columns: blocks s and 4 + s of a superblock, whose codes are in LDS for its four steps.  A sub-step is eight columns of
+            // both blocks; its weights are converted in the sub-step before.
+            uint32_t scales[4], scales_next[4];
+            float sc[4];
+            u32x4 codes[4], fx[2][2];
+            bf16x8 fw[2][4];
+            auto fetch_scales = [&](uint32_t super) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) scales_next[j] = w_scales(j, super);
+            };
+            auto scales_arrive = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(scales_next[j]));
+            };
+            fetch_scales(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { fetch_w(i, 0); fetch_x(i, 0, 0, 0); }
+            wait_loads<0>();
+            scales_arrive();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scales[j] = scales_next[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fetch_x(i, 0, 1, 1);
+            __syncthreads();
+            if constexpr (act > 0) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) codes[j] = read_w(j, 0, 0);
+#pragma unroll
+                for (int i = 0; i < act; ++i) fx[0][i] = read_x(i, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sc[j] = scale_operand(scales[j] & 255);
+                    fw[0][j] = codes_bf16(codes[j][0], sc[j]);
+                }
+            }
+            // MORE: another superblock follows
+            auto step = [&](auto S, auto MORE, uint32_t super) __attribute__((always_inline)) {
+                constexpr int s = decltype(S)::value;
+                constexpr bool load_w = decltype(MORE)::value != 0, next = load_w || s < 3, load = load_w || s < 2;
+                constexpr uint32_t stage = s & 1;
+                auto sub = [&](auto KS) __attribute__((always_inline)) {
+                    constexpr int ks = decltype(KS)::value, set = ks & 1;
+                    if constexpr (!load_w && act > 0) {      // 0 for blocks past the end, on both sides: a row may hold what is not finite
+                        const uint32_t mask = super * 8 + 4 * h + s < blocks ? ~0u : 0u;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const u32x4 v = __builtin_bit_cast(u32x4, fw[set][j]);
+                            fw[set][j] = __builtin_bit_cast(bf16x8, u32x4{v[0] & mask, v[1] & mask, v[2] & mask, v[3] & mask});
+                        }
+#pragma unroll
+                        for (int i = 0; i < act; ++i)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) fx[set][i][c] &= mask;
+                    }
+                    if constexpr (ks == 3) {
+                        if constexpr (next && act > 0) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) codes[j] = read_w(j, (s + 1) % 4, (super + (s == 3)) & 1);
+#pragma unroll
+                            for (int i = 0; i < act; ++i) fx[set ^ 1][i] = read_x(i, 0, stage ^ 1);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        const int i = n / 4, j = n % 4;
+                        if (i < act) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), fw[set][j], acc[i][j], 0, 0, 0);
+                        if constexpr (ks < 3) {
+                            if (n < act) fx[set ^ 1][n] = read_x(n, ks + 1, stage);
+                            if (act > 0 && (n & 1)) fw[set ^ 1][n / 2] = codes_bf16(codes[n / 2][ks + 1], sc[n / 2]);
+                            // the next superblock's weights, in the first two steps of this one
+                            if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
+                        } else {
+                            if (load && (n & 1)) fetch_x(n / 2, super + (s + 2) / 4, (s + 2) % 4, stage);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if constexpr (ks == 3) {
+                        if constexpr (s == 3) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) scales[j] = scales_next[j];
+                        }
+                        if constexpr (next && act > 0) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                sc[j] = scale_operand((scales[j] >> (8 * ((s + 1) % 4))) & 255);
+                                fw[set ^ 1][j] = codes_bf16(codes[j][0], sc[j]);
+                            }
+                        }
+                    }
+                };
+                if (s == 0 && load_w) fetch_scales(super + 1);
+                sub(Int<0>{});
+                sub(Int<1>{});
+                sub(Int<2>{});
+                // all but the two loads of weights that this step issued
+                if (s < 2 && load_w) wait_loads<2>();
+                else wait_loads<0>();
+                if (s == 2) scales_arrive();
+                __syncthreads();
+                sub(Int<3>{});
+            };
+            uint32_t super = 0;
+            for (; super + 1 < supers; ++super) {
+                step(Int<0>{}, Int<1>{}, super);
+                step(Int<1>{}, Int<1>{}, super);
+                step(Int<2>{}, Int<1>{}, super);
+                step(Int<3>{}, Int<1>{}, super);
+            }
+            step(Int<0>{}, Int<0>{}, super);
+            step(Int<1>{}, Int<0>{}, super);
+            step(Int<2>{}, Int<0>{}, super);
+            step(Int<3>{}, Int<0>{}, super);
+        }
+    };
+    // (the same for a whole wavefront)
+    if (wm * 32 + 128 < t.rows) k_loop(Int<2>{});
+    else if (wm * 32 < t.rows) k_loop(Int<1>{});
+    else k_loop(Int<0>{});
+
+    // Column q of a 32 x 32 result lies in lane q and q + 32, its rows 8 (r / 4) + 4 h + r % 4 in their 16 numbers.  For BF16 neighbouring
+    // lanes swap numbers, so that an even lane has two columns of an even row and an odd one of the next: 4-byte stores.
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t row0 = (wm + 4 * i) * 32 + 4 * h;
+        if ((wm + 4 * i) * 32 >= t.rows) break;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+            if constexpr (sizeof(OUT) == 2) {
+                const uint32_t row = row0 + 8 * (r / 4) + r % 4 + (q & 1);
+                char* const dst = static_cast<char*>(a.out) + uint64_t(t.first + min(row, t.rows - 1)) * a.out_stride;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t mine = pack_bf16_rne(acc[i][j][r], acc[i][j][r + 1]), other = dpp<kDppXor1>(mine);
+                    const uint32_t both = __builtin_amdgcn_perm(other, mine, (q & 1) ? 0x03020706u : 0x05040100u);
+                    const uint32_t n = n0 + wn * 128 + j * 32 + (q & ~1u);
+                    if (row >= t.rows || n >= a.N) continue;
+                    if (a.out_vec && n + 1 < a.N) {
+                        *reinterpret_cast<uint32_t*>(dst + 2 * n) = both;
+                    } else {
+                        reinterpret_cast<uint16_t*>(dst)[n] = uint16_t(both);
+                        if (n + 1 < a.N) reinterpret_cast<uint16_t*>(dst)[n + 1] = uint16_t(both >> 16);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t row = row0 + 8 * (r / 4) + (r + c) % 4;
+                    if (row >= t.rows) continue;
+                    float* const dst = reinterpret_cast<float*>(static_cast<char*>(a.out) + uint64_t(t.first + row) * a.out_stride);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t n = n0 + wn * 128 + j * 32 + q;
+                        if (n < a.N) dst[n] = acc[i][j][r + c];
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <bool MX, typename OUT>
+void go(const MxProductArgs& a, hipStream_t stream) {
+    const WideGrid grid(a.cap / kTile + (a.cap < a.E ? a.cap : a.E), a.N);
+    const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
+    const bool whole = words(a.ws, a.K / kMxBlock) && (!MX || words(a.row_scales, a.row_scales_stride));
+    const dim3 wgs(grid.total), threads(kThreads);
+    constexpr uint32_t lds = 4 * kStage + 4 * kTileWords;
+    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MX, true, OUT>), wgs, threads, lds, stream, a, grid);
+    else hipLaunchKernelGGL((mx_wide_kernel<MX, false, OUT>), wgs, threads, lds, stream, a, grid);
+}
+
+}  // namespace
+
+// Rows at 16-byte addresses, a tile's places within 31 bits, and a launch of less than 2^31 threads.
+bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) {
+    return a.rows_vec && a.row_stride < (1u << 23) && (!mx_rows || a.row_scales_stride < (1u << 22)) &&
+           (a.cap / kTile + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(a.N) + kTile - 1) / kTile + 8) < (1u << 21);
+}
+
+hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream) {
+    if (mx_rows) out_f32 ? go<true, float>(a, stream) : go<true, bf16_t>(a, stream);
+    else out_f32 ? go<false, float>(a, stream) : go<false, bf16_t>(a, stream);
+    return hipGetLastError();
+}
+
+}  // namespace fluxmoe
