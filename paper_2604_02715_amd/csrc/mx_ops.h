@@ -54,6 +54,8 @@ hipError_t launch_mx_product(const MxProductArgs& a, bool mx_rows, bool out_f32,
 // 256 x 256 tiles (mx_tiles.hip)
 bool mx_wide_takes(const MxProductArgs& a, bool mx_rows);
 hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream);
+bool mx_wide_grad_takes(const MxProductArgs& a);
+hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream);
 hipError_t launch_mx_product_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream);
 
 }  // namespace fluxmoe

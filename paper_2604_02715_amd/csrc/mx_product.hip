@@ -278,6 +278,7 @@ hipError_t launch_mx_product(const MxProductArgs& a, bool mx_rows, bool out_f32,
     return out_f32 ? product<float>(a, mx_rows, stream) : product<bf16_t>(a, mx_rows, stream);
 }
 hipError_t launch_mx_product_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream) {
+    if (a.cap / a.E > 32 && mx_wide_grad_takes(a)) return launch_mx_wide_grad(a, out_f32, stream);
     if (out_f32) go_tile<true, float>(a, stream);
     else go_tile<true, bf16_t>(a, stream);
     return hipGetLastError();

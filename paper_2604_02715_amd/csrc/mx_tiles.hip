@@ -15,6 +15,8 @@ namespace {
 constexpr uint32_t kTile = 256;
 constexpr int kStage = 32768;                            // 256 rows of 128 bytes
 constexpr uint32_t kThreads = 512;
+constexpr uint32_t kScaleRow = 260;                      // words between the gradient's scales of two blocks of columns: in different banks
+constexpr int kScaleStage = 8 * kScaleRow * 4;
 
 // Where a workgroup's tile lies.  Workgroups go to the eight XCDs in turn; the 32 that run on one at a time take a super-tile of
 // 32 >> sn_log2 row tiles by 1 << sn_log2 strips, whose rows and weights they share in that XCD's L2.
@@ -61,43 +63,59 @@ __device__ __forceinline__ uint32_t four_scales(row_t m, uint32_t row, uint32_t 
 template <int N>
 using Int = std::integral_constant<int, N>;
 
+// What is multiplied: rows in 4 bits or BF16 by weights, summed over their columns; or for the gradient BF16 rows of d_out by weights turned
+// round, summed over the outputs.  "Columns" below are those of the result, n0 the tile's first.
+enum Mode { kMxRows, kBf16Rows, kGradRows };
+
 // WHOLE: scales are read four at a time
-template <bool MX, bool WHOLE, typename OUT>
+template <Mode MODE, bool WHOLE, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, WideGrid grid) {
-    extern __shared__ __align__(16) uint8_t lds[];           // rows' two stages, weights' two stages, find_tile's words
+    constexpr bool MX = MODE == kMxRows, GRAD = MODE == kGradRows;
+    extern __shared__ __align__(16) uint8_t lds[];           // rows' two stages, weights' two stages, the gradient's scales twice, find_tile's words
     uint32_t row_tile, strip;
     if (!grid.locate(blockIdx.x, row_tile, strip)) return;
-    const Tile t = find_tile<kThreads>(a, kTile, row_tile, reinterpret_cast<uint32_t*>(lds + 4 * kStage));
+    const Tile t = find_tile<kThreads>(a, kTile, row_tile, reinterpret_cast<uint32_t*>(lds + 4 * kStage + (GRAD ? 2 * kScaleStage : 0)));
     if (t.rows == 0) return;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t wm = wave >> 1, wn = wave & 1, q = lane & 31, h = lane >> 5;
-    const uint32_t n0 = strip * kTile, blocks = a.K / kMxBlock, supers = (blocks + 7) / 8;
+    const uint32_t n0 = strip * kTile, blocks = a.K / kMxBlock;
+    const uint32_t outs = GRAD ? a.K : a.N, supers = GRAD ? (a.N + 255) / 256 : (blocks + 7) / 8;
     const uint32_t lds_base = uint32_t(uintptr_t((__attribute__((address_space(3))) void*)lds));
 
     // What the lane fetches: four KiB of each operand to a wavefront and stage, rows 8 (4 wave + i) + lane / 8.
     const uint8_t* const x_base = static_cast<const uint8_t*>(a.rows) + uint64_t(t.first) * a.row_stride;
-    const uint8_t* const w_base = a.w + (uint64_t(t.expert) * a.N + n0) * (a.K / 2);
+    const uint8_t* const w_base = a.w + (uint64_t(t.expert) * a.N + (GRAD ? 0 : n0)) * (a.K / 2) + (GRAD ? n0 / 2 : 0);
     uint32_t x_off[4], w_off[4];                             // of the rows
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t row = 8 * (wave * 4 + i) + (lane >> 3);
         x_off[i] = min(row, t.rows - 1) * uint32_t(a.row_stride);
-        w_off[i] = min(row, a.N - 1 - n0) * (a.K / 2);
+        w_off[i] = GRAD ? row : min(row, a.N - 1 - n0) * (a.K / 2);
     }
     auto piece_of = [&](int i) __attribute__((always_inline)) { return (lane & 7) ^ ((4 * (i & 1) + (lane >> 4)) & 7); };
     // Past the end of a row its last block is fetched in place of those that are missing, whose weights become 0 ahead of their products.
     auto fetch_w = [&](int i, uint32_t super) __attribute__((always_inline)) {
+        if constexpr (GRAD) {                                // 256 outputs of the strip's eight blocks of columns
+            load_to_lds(w_base + uint64_t(super) * 256 * (a.K / 2),
+                        min(w_off[i], a.N - 1 - super * 256) * (a.K / 2) + min((lane & 7) ^ (4 * (wave & 1)), (a.K - n0) / kMxBlock - 1) * 16,
+                        lds_base + (2 + (super & 1)) * kStage + (wave * 4 + i) * 1024);
+            return;
+        }
         load_to_lds(w_base + uint64_t(super) * 128, w_off[i] + min(piece_of(i), blocks - 1 - super * 8) * 16,
                     lds_base + (2 + (super & 1)) * kStage + (wave * 4 + i) * 1024);
     };
     // the rows' codes of a superblock, or BF16 columns of its blocks s and 4 + s, into stage `to`
     auto fetch_x = [&](int i, uint32_t super, uint32_t s, uint32_t to) __attribute__((always_inline)) {
+        if constexpr (GRAD) {                                // 64 outputs of a superblock's 256
+            load_to_lds(x_base, x_off[i] + min(super * 32 + s * 8 + piece_of(i), a.N / 8 - 1) * 16, lds_base + to * kStage + (wave * 4 + i) * 1024);
+            return;
+        }
         const uint32_t block = min(MX ? piece_of(i) : s + 4 * (piece_of(i) >> 2), blocks - 1 - super * 8);
         load_to_lds(x_base + uint64_t(super) * (MX ? 128 : 512), x_off[i] + block * (MX ? 16 : 64) + (MX ? 0 : (piece_of(i) & 3) * 16),
                     lds_base + to * kStage + (wave * 4 + i) * 1024);
     };
 
-    const row_t ws_at = bytes_at(a.ws, (uint64_t(t.expert) * a.N + n0) * blocks, min(kTile, a.N - n0) * blocks);
+    const row_t ws_at = bytes_at(a.ws, (uint64_t(t.expert) * a.N + n0) * blocks, GRAD ? 0 : min(kTile, a.N - n0) * blocks);
     const row_t xs_at = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
     auto w_scales = [&](int j, uint32_t super) __attribute__((always_inline)) {
         return four_scales<WHOLE>(ws_at, min(wn * 128 + j * 32 + q, a.N - 1 - n0) * blocks, super * 8 + 4 * h, blocks);
@@ -211,6 +229,122 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             for (; super + 2 < supers; ++super) step(Int<1>{}, Int<1>{}, super);
             if (super + 1 < supers) step(Int<1>{}, Int<0>{}, super++);
             step(Int<0>{}, Int<0>{}, super);
+        } else if constexpr (GRAD) {
+            // A superblock is 256 outputs, a step 64 of them, a sub-step eight of either half of those.  Lane q has four neighbouring columns, a 32 x 32 tile
+            // every fourth one: two bytes of codes of each of eight outputs become the tiles' fragments by a conversion and a permutation to
+            // each two numbers.  The scales lie in LDS as the conversion takes them, a block's outputs one after the other.
+            uint32_t scales_next = 0;
+            u32x4 fx[2][2], fw[2][4], sc[2];
+            uint32_t raw[8], pair[8][2];
+            const uint32_t raw_at = 2 * kStage + h * 4096 + 16 * ((wn * 4 + q / 8) ^ (4 * h)) + 2 * (q & 7);
+            const uint32_t sc_at = 4 * kStage + ((wn * 4 + q / 8) * kScaleRow + 32 * h) * 4;
+            auto fetch_scales = [&](uint32_t super) __attribute__((always_inline)) {
+                const row_t m = bytes_at(a.ws, (uint64_t(t.expert) * a.N + super * 256) * blocks, min(a.N - super * 256, 256u) * blocks);
+                scales_next = four_scales<WHOLE>(m, (tid >> 1) * blocks, n0 / kMxBlock + 4 * (tid & 1), blocks);
+            };
+            auto put_scales = [&](uint32_t super) __attribute__((always_inline)) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<float*>(lds + 4 * kStage + (super & 1) * kScaleStage + ((4 * (tid & 1) + b) * kScaleRow + (tid >> 1)) * 4) =
+                        scale_operand((scales_next >> (8 * b)) & 255);
+            };
+            auto read_raw = [&](uint32_t super, int s, int ks) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) raw[j] = *reinterpret_cast<const uint16_t*>(lds + (raw_at + (super & 1) * kStage) + (64 * s + 8 * ks + j) * 128);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) sc[j] = read(sc_at + (super & 1) * kScaleStage + (64 * s + 8 * ks + 4 * j) * 4);
+            };
+            auto convert = [&](int j) __attribute__((always_inline)) {
+                const float scale = __uint_as_float(sc[j / 4][j % 4]);
+                pair[j][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw[j], scale, 0));
+                pair[j][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw[j], scale, 1));
+            };
+            auto turn = [&](int set, int c) __attribute__((always_inline)) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    fw[set][c][d] = __builtin_amdgcn_perm(pair[2 * d + 1][c / 2], pair[2 * d][c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
+            };
+            fetch_scales(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { fetch_w(i, 0); fetch_x(i, 0, 0, 0); }
+            wait_loads<0>();
+            asm volatile("" : "+v"(scales_next));
+            put_scales(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fetch_x(i, 0, 1, 1);
+            __syncthreads();
+            if constexpr (act > 0) {
+                read_raw(0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < act; ++i) fx[0][i] = read_x(i, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) convert(j);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) turn(0, c);
+            }
+            auto step = [&](auto S, auto MORE, uint32_t super) __attribute__((always_inline)) {
+                constexpr int s = decltype(S)::value;
+                constexpr bool load_w = decltype(MORE)::value != 0, next = load_w || s < 3, load = load_w || s < 2;
+                constexpr uint32_t stage = s & 1;
+                auto sub = [&](auto KS) __attribute__((always_inline)) {
+                    constexpr int ks = decltype(KS)::value, set = ks & 1;
+                    constexpr bool ahead = act > 0 && (ks < 3 || next);
+                    if constexpr (!load_w && act > 0) {      // 0 past the last output, on both sides
+                        const uint32_t mask = super * 256 + 64 * s + 32 * h + 8 * ks < a.N ? ~0u : 0u;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) fw[set][j][c] &= mask;
+#pragma unroll
+                            for (int i = 0; i < act; ++i) fx[set][i][c] &= mask;
+                        }
+                    }
+                    if constexpr (ahead) {
+                        if (ks < 3) read_raw(super, s, ks + 1);
+                        else read_raw(super + (s == 3), (s + 1) % 4, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        const int i = n / 4, j = n % 4;
+                        if (i < act) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), __builtin_bit_cast(bf16x8, fw[set][j]), acc[i][j], 0, 0, 0);
+                        if constexpr (ahead) {
+                            if (n < act) fx[set ^ 1][n] = ks < 3 ? read_x(n, ks + 1, stage) : read_x(n, 0, stage ^ 1);
+                            if (n == 2 || n == 3)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) convert(4 * (n - 2) + k);
+                            if (n >= 4) turn(set ^ 1, n - 4);
+                        }
+                        // the next superblock's weights, in the first two steps of this one
+                        if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
+                        if (ks == 3 && load && (n & 1)) fetch_x(n / 2, super + (s + 2) / 4, (s + 2) % 4, stage);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                if constexpr (s == 0 && load_w) fetch_scales(super + 1);
+                sub(Int<0>{});
+                sub(Int<1>{});
+                sub(Int<2>{});
+                if constexpr (s < 2 && load_w) wait_loads<2>();       // all but the two loads of weights that this step issued
+                else wait_loads<0>();
+                if constexpr (s == 2 && load_w) {
+                    asm volatile("" : "+v"(scales_next));
+                    put_scales(super + 1);                            // read behind the next step's barrier
+                }
+                __syncthreads();
+                sub(Int<3>{});
+            };
+            uint32_t super = 0;
+            for (; super + 1 < supers; ++super) {
+                step(Int<0>{}, Int<1>{}, super);
+                step(Int<1>{}, Int<1>{}, super);
+                step(Int<2>{}, Int<1>{}, super);
+                step(Int<3>{}, Int<1>{}, super);
+            }
+            step(Int<0>{}, Int<0>{}, super);
+            step(Int<1>{}, Int<0>{}, super);
+            step(Int<2>{}, Int<0>{}, super);
+            step(Int<3>{}, Int<0>{}, super);
         } else {
             // A step is 64 columns: blocks s and 4 + s of a superblock, whose codes are in LDS for its four steps.  A sub-step is eight columns of
             // both blocks; its weights are converted in the sub-step before.
@@ -338,6 +472,25 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     for (int i = 0; i < 2; ++i) {
         const uint32_t row0 = (wm + 4 * i) * 32 + 4 * h;
         if ((wm + 4 * i) * 32 >= t.rows) break;
+        if constexpr (GRAD) {                                // the lane's four columns are those of the four tiles
+            const uint32_t n = n0 + wn * 128 + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t row = row0 + 8 * (r / 4) + r % 4;
+                if (row >= t.rows || n >= outs) continue;
+                OUT* const dst = reinterpret_cast<OUT*>(static_cast<char*>(a.out) + uint64_t(t.first + row) * a.out_stride) + n;
+                if (a.out_vec) {
+                    if constexpr (sizeof(OUT) == 2)
+                        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16_rne(acc[i][0][r], acc[i][1][r]), pack_bf16_rne(acc[i][2][r], acc[i][3][r]));
+                    else
+                        *reinterpret_cast<float4*>(dst) = make_float4(acc[i][0][r], acc[i][1][r], acc[i][2][r], acc[i][3][r]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) from_float(dst + j, acc[i][j][r]);
+                }
+            }
+            continue;
+        }
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
             if constexpr (sizeof(OUT) == 2) {
@@ -373,28 +526,34 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     }
 }
 
-template <bool MX, typename OUT>
+template <Mode MODE, typename OUT>
 void go(const MxProductArgs& a, hipStream_t stream) {
-    const WideGrid grid(a.cap / kTile + (a.cap < a.E ? a.cap : a.E), a.N);
+    const WideGrid grid(a.cap / kTile + (a.cap < a.E ? a.cap : a.E), MODE == kGradRows ? a.K : a.N);
     const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
-    const bool whole = words(a.ws, a.K / kMxBlock) && (!MX || words(a.row_scales, a.row_scales_stride));
+    const bool whole = words(a.ws, a.K / kMxBlock) && (MODE != kMxRows || words(a.row_scales, a.row_scales_stride));
     const dim3 wgs(grid.total), threads(kThreads);
-    constexpr uint32_t lds = 4 * kStage + 4 * kTileWords;
-    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MX, true, OUT>), wgs, threads, lds, stream, a, grid);
-    else hipLaunchKernelGGL((mx_wide_kernel<MX, false, OUT>), wgs, threads, lds, stream, a, grid);
+    constexpr uint32_t lds = 4 * kStage + (MODE == kGradRows ? 2 * kScaleStage : 0) + 4 * kTileWords;
+    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, true, OUT>), wgs, threads, lds, stream, a, grid);
+    else hipLaunchKernelGGL((mx_wide_kernel<MODE, false, OUT>), wgs, threads, lds, stream, a, grid);
+}
+
+bool fits(const MxProductArgs& a, uint32_t outs) {           // places within 31 bits, and a launch of less than 2^31 threads
+    return a.rows_vec && a.row_stride < (1u << 23) && (a.cap / kTile + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(outs) + kTile - 1) / kTile + 8) < (1u << 21);
 }
 
 }  // namespace
 
-// Rows at 16-byte addresses, a tile's places within 31 bits, and a launch of less than 2^31 threads.
-bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) {
-    return a.rows_vec && a.row_stride < (1u << 23) && (!mx_rows || a.row_scales_stride < (1u << 22)) &&
-           (a.cap / kTile + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(a.N) + kTile - 1) / kTile + 8) < (1u << 21);
+bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) { return fits(a, a.N) && (!mx_rows || a.row_scales_stride < (1u << 22)); }
+hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream) {
+    if (mx_rows) out_f32 ? go<kMxRows, float>(a, stream) : go<kMxRows, bf16_t>(a, stream);
+    else out_f32 ? go<kBf16Rows, float>(a, stream) : go<kBf16Rows, bf16_t>(a, stream);
+    return hipGetLastError();
 }
 
-hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream) {
-    if (mx_rows) out_f32 ? go<true, float>(a, stream) : go<true, bf16_t>(a, stream);
-    else out_f32 ? go<false, float>(a, stream) : go<false, bf16_t>(a, stream);
+// (d_out's rows are whole 16-byte pieces: of one that reaches past a row's end the rest would be multiplied)
+bool mx_wide_grad_takes(const MxProductArgs& a) { return fits(a, a.K) && a.N % 8 == 0; }
+hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream) {
+    out_f32 ? go<kGradRows, float>(a, stream) : go<kGradRows, bf16_t>(a, stream);
     return hipGetLastError();
 }
 
