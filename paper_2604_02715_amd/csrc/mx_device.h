@@ -1,6 +1,8 @@
 // Device code shared by the products with experts' weights in 4-bit floating point.
 #pragma once
 
+#include <type_traits>
+
 #include "block_device.h"
 #include "mx_ops.h"
 
@@ -79,5 +81,49 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t codes, float scale) {
                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
     return __builtin_bit_cast(bf16x8, v);
 }
+
+// The four scales of blocks `at` .. `at` + 3 of a row of `blocks` that lies `row` bytes into m, 0 past its end.  WHOLE: they are whole words.
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t four_scales(row_t m, uint32_t row, uint32_t at, uint32_t blocks) {
+    if constexpr (WHOLE) return __builtin_amdgcn_raw_buffer_load_b32(m, at < blocks ? row + at : kNowhere, 0, kCached);
+    uint32_t v[4];
+#pragma unroll
+    for (uint32_t b = 0; b < 4; ++b) v[b] = __builtin_amdgcn_raw_buffer_load_b8(m, at + b < blocks ? row + at + b : kNowhere, 0, kCached);
+    return v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24;
+}
+
+// The scales of blocks block, block + 4, block + 8, block + 12 of such a row, block being q (0 .. 3) past a multiple of 16.
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t spread_scales(row_t m, uint32_t row, uint32_t block, uint32_t q, uint32_t blocks) {
+    uint32_t v[4];
+    if constexpr (WHOLE) {
+        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(m, row + (block - q), 0, kCached);
+        const uint32_t two = 0x0C0C0400u + q * 0x0101u;  // byte q of either word
+        uint32_t s = __builtin_amdgcn_perm(w[1], w[0], two) | __builtin_amdgcn_perm(w[3], w[2], two) << 16;
+        // the words past a row's end are the next row's
+        const uint32_t left = blocks - min(blocks, block), here = min((left + 3) / 4, 4u);
+        return here == 4 ? s : s & ((1u << (8 * here)) - 1);
+    }
+#pragma unroll
+    for (uint32_t b = 0; b < 4; ++b) v[b] = __builtin_amdgcn_raw_buffer_load_b8(m, block + 4 * b < blocks ? row + block + 4 * b : kNowhere, 0, kCached);
+    return v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24;
+}
+
+// The scales of blocks block and block + 4, block being q (0 .. 3) past a multiple of 8.
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t pair_scales(row_t m, uint32_t row, uint32_t block, uint32_t q, uint32_t blocks) {
+    if constexpr (WHOLE) {
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(m, row + (block - q), 0, kCached);
+        const uint32_t s = __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0400u + q * 0x0101u);
+        return block + 4 < blocks ? s : block < blocks ? s & 255 : 0;            // the words past a row's end are the next row's
+    }
+    uint32_t v[2];
+#pragma unroll
+    for (uint32_t b = 0; b < 2; ++b) v[b] = __builtin_amdgcn_raw_buffer_load_b8(m, block + 4 * b < blocks ? row + block + 4 * b : kNowhere, 0, kCached);
+    return v[0] | v[1] << 8;
+}
+
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 }  // namespace fluxmoe

@@ -50,19 +50,6 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
-// The four scales of blocks `at` .. `at` + 3 of a row of `blocks` that lies `row` bytes into m, 0 past its end.  WHOLE: they are whole words.
-template <bool WHOLE>
-__device__ __forceinline__ uint32_t four_scales(row_t m, uint32_t row, uint32_t at, uint32_t blocks) {
-    if constexpr (WHOLE) return __builtin_amdgcn_raw_buffer_load_b32(m, at < blocks ? row + at : kNowhere, 0, kCached);
-    uint32_t v[4];
-#pragma unroll
-    for (uint32_t b = 0; b < 4; ++b) v[b] = __builtin_amdgcn_raw_buffer_load_b8(m, at + b < blocks ? row + at + b : kNowhere, 0, kCached);
-    return v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24;
-}
-
-template <int N>
-using Int = std::integral_constant<int, N>;
-
 // What is multiplied: rows in 4 bits or BF16 by weights, summed over their columns; or for the gradient BF16 rows of d_out by weights turned
 // round, summed over the outputs.  "Columns" below are those of the result, n0 the tile's first.
 enum Mode { kMxRows, kBf16Rows, kGradRows };
