@@ -175,9 +175,8 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
 // the weights of the next 256 columns are on their way while these are multiplied: loads return in the order of their issue, so rows that a
 // wavefront fetched for itself would be waited for behind those weights.  A row's 16-byte pieces are placed so that 16 rows' pieces of one
 // number lie in different banks.
-template <int MI, bool MX, bool WHOLE, typename OUT>
+template <int MI, int NI, bool MX, bool WHOLE, typename OUT>
 __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
-    constexpr int NI = 4;
     constexpr uint32_t kPieces = MX ? 8 : 32;                // 16-byte pieces of a row's 256 columns
     constexpr int kMine = (16 * MI * kPieces + kThreads - 1) / kThreads;      // that a thread brings to LDS
     __shared__ uint32_t s_tile[kTileWords];
@@ -189,7 +188,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
         const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
         const Tile t = find_tile<kThreads>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;
-        const uint32_t n0 = strip * 256 + wave * 64, outs = n0 < a.N ? min(a.N - n0, 64u) : 0;
+        const uint32_t n0 = (strip * 4 + wave) * (16 * NI), outs = n0 < a.N ? min(a.N - n0, uint32_t(16 * NI)) : 0;
         const uint64_t w_row = uint64_t(t.expert) * a.N + min(n0, a.N - 1);
         const row_t w = bytes_at(a.w, w_row * (a.K / 2), outs * (a.K / 2)), ws = bytes_at(a.ws, w_row * blocks, outs * blocks);
         const row_t x = bytes_at(a.rows, uint64_t(t.first) * a.row_stride, (t.rows - 1) * uint32_t(a.row_stride) + (MX ? a.K / 2 : a.K * 2));
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
             wave_fence();
 #pragma unroll
             for (int c = 0; c < NI; ++c) {
-                const uint32_t row = c * 4 + lane / 16, quad = lane % 16;
+                const uint32_t row = (c * 64 + lane) / (4 * NI), quad = lane % (4 * NI);
                 const f32x4 v = s_acc[wave][quad >> 2][(quad & 3) * 16 + row];
                 if (m * 16 + row >= t.rows || quad * 4 >= outs) continue;
                 store_outputs<OUT>(a, t.first + m * 16 + row, n0 + quad * 4, min(outs - quad * 4, 4u), v);
@@ -307,18 +306,18 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
     }
 }
 
-// The gradient likewise.  A workgroup has 16 MI rows and 256 columns, its wavefronts a quarter of the outputs each, 32 at a time.  Lane (r, q)
+// The gradient likewise.  A workgroup has 16 MI rows and 256 columns, its four or eight wavefronts share out the outputs, 32 at a time.  Lane (r, q)
 // loads 16 neighbouring columns of eight outputs, eight bytes of each, turns them into sixteen fragments of eight outputs by a conversion and
 // a permutation to each two numbers, and fragment c goes to a matrix instruction whose results are column c of every lane's.
-template <int MI, bool VEC, typename OUT>
-__global__ __launch_bounds__(kThreads) void mx_stream_grad_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
+template <int MI, int WAVES, bool VEC, typename OUT>
+__global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
     __shared__ uint32_t s_tile[kTileWords];
-    __shared__ f32x4 s_acc[3][MI][16][64];
+    __shared__ f32x4 s_acc[WAVES - 1][16][64];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
     const uint32_t blocks = a.K / kMxBlock, chunks = (a.N + 31) / 32;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
-        const Tile t = find_tile<kThreads>(a, 16 * MI, tile_at, s_tile);
+        const Tile t = find_tile<64 * WAVES>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;
         const uint32_t k0 = strip * 256, column = k0 + r * 16;
         f32x4 acc[MI][16];
@@ -326,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void mx_stream_grad_kernel(MxProductArgs 
         for (int m = 0; m < MI; ++m)
 #pragma unroll
             for (int c = 0; c < 16; ++c) acc[m][c] = f32x4{0, 0, 0, 0};
-        for (uint32_t chunk = wave; chunk < chunks; chunk += 4) {
+        for (uint32_t chunk = wave; chunk < chunks; chunk += WAVES) {
             const uint64_t row = uint64_t(t.expert) * a.N + chunk * 32;
             const uint32_t left = min(a.N - chunk * 32, 32u);
             const row_t w = bytes_at(a.w, row * (a.K / 2), left * (a.K / 2)), ws = bytes_at(a.ws, row * blocks, left * blocks);
@@ -375,33 +374,27 @@ __global__ __launch_bounds__(kThreads) void mx_stream_grad_kernel(MxProductArgs 
                 }
             }
         }
-        // The quarters' sums in their order.  A lane then has 16 neighbouring columns of four lanes' for row r: the wavefronts take four of them each.
-        if (wave) {
+        // The wavefronts' sums in their order, 16 rows at a time; a lane then has 16 neighbouring columns of four lanes' for its row.
 #pragma unroll
-            for (int m = 0; m < MI; ++m)
+        for (int m = 0; m < MI; ++m) {
+            if (m) __syncthreads();
+            if (wave) {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) s_acc[wave - 1][m][c][lane] = acc[m][c];
-        }
-        __syncthreads();
-        if (wave == 0) {
+                for (int c = 0; c < 16; ++c) s_acc[wave - 1][c][lane] = acc[m][c];
+            }
+            __syncthreads();
+            if (wave != 0 || m * 16 + r >= t.rows) continue;
 #pragma unroll
-            for (int m = 0; m < MI; ++m) {
+            for (int c = 0; c < 16; ++c)
 #pragma unroll
-                for (int c = 0; c < 16; ++c)
+                for (int k = 0; k < WAVES - 1; ++k) acc[m][c] += s_acc[k][c][lane];
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) acc[m][c] += s_acc[k][m][c][lane];
-                if (m * 16 + r < t.rows) {
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t k = k0 + (4 * q + i) * 16;
+                if (k >= a.K) continue;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t k = k0 + (4 * q + i) * 16;
-                        if (k >= a.K) continue;
-#pragma unroll
-                        for (int c = 0; c < 16; c += 4) {
-                            const f32x4 v = {acc[m][c][i], acc[m][c + 1][i], acc[m][c + 2][i], acc[m][c + 3][i]};
-                            store_outputs<OUT>(a, t.first + m * 16 + r, k + c, 4, v);
-                        }
-                    }
-                }
+                for (int c = 0; c < 16; c += 4)
+                    store_outputs<OUT>(a, t.first + m * 16 + r, k + c, 4, f32x4{acc[m][c][i], acc[m][c + 1][i], acc[m][c + 2][i], acc[m][c + 3][i]});
             }
         }
     }
@@ -553,7 +546,12 @@ void go_stream(const MxProductArgs& a, hipStream_t stream) {
 template <int MI, bool VEC, typename OUT>
 void go_stream_grad(const MxProductArgs& a, hipStream_t stream) {
     const Plan p(a, 16 * MI, a.K, 256);
-    hipLaunchKernelGGL((mx_stream_grad_kernel<MI, VEC, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+    // Eight wavefronts where there are fewer than four workgroups for a CU: 160 experts, 13 rows each, 1536 columns 185 -> 162 us, 8 experts, 16 rows,
+    // 4096 columns of 28672 outputs 369 -> 217; with more workgroups the longer sum at the end costs more (512 experts, 512 columns 90 -> 95).
+    if (std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E)) * p.strips < 4 * 256)
+        hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 8, VEC, OUT>), dim3(p.grid), dim3(512), 0, stream, a, p.strips, p.items);
+    else
+        hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 4, VEC, OUT>), dim3(p.grid), dim3(256), 0, stream, a, p.strips, p.items);
 }
 template <bool GRAD, typename OUT>
 void go_tile(const MxProductArgs& a, hipStream_t stream) {
@@ -561,37 +559,59 @@ void go_tile(const MxProductArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((mx_tile_kernel<GRAD, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
 }
 
-template <int MI, bool MX, typename OUT>
+template <int MI, int NI, bool MX, typename OUT>
 void go_strip(const MxProductArgs& a, bool whole, hipStream_t stream) {
-    const Plan p(a, 16 * MI, a.N, 256);
-    if (whole) hipLaunchKernelGGL((mx_strip_kernel<MI, MX, true, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
-    else hipLaunchKernelGGL((mx_strip_kernel<MI, MX, false, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+    const Plan p(a, 16 * MI, a.N, 64 * NI);
+    if (whole) hipLaunchKernelGGL((mx_strip_kernel<MI, NI, MX, true, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+    else hipLaunchKernelGGL((mx_strip_kernel<MI, NI, MX, false, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
 }
 
-#ifndef STRIP_MIN
-#define STRIP_MIN 192
-#endif
-// The widest workgroups of which there are enough
+// Which of the three. Times in us, 16-bit outputs, even routing but for 512 experts:
+//   rows in 4 bits, side by side / quarters: 512 columns (512 experts, 900 tokens) 88 / 203, 1536 (160, 256) 143 / 167, 2048 (512, 256) 100 / 106,
+//   4096 (8, 64) 154 / 134, 5120 (160, 16) 151 / 116: long rows are better read a whole piece at a time, and there are more workgroups;
+//   BF16 rows, which quarters fetch for every 64 outputs: 1536 (160, 256) 153 / 253, 5120 (160, 16) 145 / 156;
+//   BF16 rows, 32 / 64 outputs to a wavefront: one tile of rows 153 / 159 (1536), 145 / 155 (5120), two 176 / 171.
+// Where the workgroups would be few, narrow ones with a quarter each (one token of 512 experts, 2048 columns, 1024 outputs 7.7).
 template <int MI, bool MX, typename OUT>
 void pick_stream(const MxProductArgs& a, hipStream_t stream) {
     const uint64_t tiles = std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E));
-    if (tiles * (a.N / 256) >= STRIP_MIN) go_strip<MI, MX, OUT>(a, whole_scales<MX>(a), stream);
+    constexpr int kStrip = MX || MI == 2 ? 4 : 2;            // sixteens of outputs to a wavefront
+    if constexpr (MI == 4) go_strip<MI, kStrip, MX, OUT>(a, whole_scales<MX>(a), stream);
+    else if ((!MX || a.K <= 2048) && tiles * (a.N / (64 * kStrip)) >= 448) go_strip<MI, kStrip, MX, OUT>(a, whole_scales<MX>(a), stream);
     else if (tiles * (a.N / 64) >= 512) go_stream<MI, 4, 4, MX, true, OUT>(a, stream);
     else go_stream<MI, 1, 4, MX, true, OUT>(a, stream);
 }
+// Two 16-row tiles of rows to a workgroup from this many rows for each expert on, on average: some experts have more than 16 then, and
+// their weights are read once (8 experts of 16 rows, 4096 columns, 28672 outputs: 156 -> 133 us, rows in 4 bits 134 -> 111; 12.8 rows level).
+constexpr uint32_t kTwoTiles = 9;
 
+// Workgroups of the wide tiles of `rows` rows; a tile is expected for each expert
+uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) { return std::max<uint64_t>(a.cap / rows, std::min(a.cap, a.E)) * ((outs + 255) / 256); }
+
+// The wide tiles take over where the matrix cores bound the call, by the rows to an expert on average. Times in us, streamed / wide tiles of 128 rows /
+// of 256, 160 experts of 1536 columns and 5120 outputs (and turned round for the gradient):
+//   rows           26               40               60               120             200
+//   4 bits         151 /  - / 207   159 /  - / 216   180 /  - / 224   279 /  - / 254  433 /  - / 311      (80: 246 / 234)
+//   BF16           171 / 215 / 278  235 / 252 / 288  292 / 269 / 308    - / 409 / 408   - / 631 / 558
+//   gradient       243 / 273 / 346  394 / 288 / 355  537 / 356 / 386    - / 504 / 447   - / 788 / 568
+// and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns (128 workgroups) 152 / 186 / 207 with BF16 rows, 200 rows
+// - / 196 / 315.
 template <typename OUT>
 hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
-    if (per_expert > 32 && mx_wide_takes(a, mx_rows)) return launch_mx_wide(a, mx_rows, sizeof(OUT) == 4, stream);
     if (mx_rows) {
+        if (per_expert > 64 && mx_wide_takes(a, true)) return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
         if (!a.rows_vec) go_stream<2, 4, 4, true, false, OUT>(a, stream);
-        else if (per_expert > 16) pick_stream<2, true, OUT>(a, stream);
+        else if (per_expert > 32) pick_stream<4, true, OUT>(a, stream);
+        else if (per_expert >= kTwoTiles) pick_stream<2, true, OUT>(a, stream);
         else pick_stream<1, true, OUT>(a, stream);
     } else {
+        if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 192 && mx_wide_takes(a, false))
+            return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 256, sizeof(OUT) == 4, stream);
         if (!a.rows_vec && per_expert > 32) go_tile<false, OUT>(a, stream);
         else if (!a.rows_vec) go_stream<1, 4, 4, false, false, OUT>(a, stream);
-        else if (per_expert > 16) pick_stream<2, false, OUT>(a, stream);
+        else if (per_expert > 32) pick_stream<4, false, OUT>(a, stream);
+        else if (per_expert >= kTwoTiles) pick_stream<2, false, OUT>(a, stream);
         else pick_stream<1, false, OUT>(a, stream);
     }
     return hipGetLastError();
@@ -600,13 +620,13 @@ hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
 template <typename OUT>
 hipError_t product_grad(const MxProductArgs& a, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
-    if (per_expert > 32) {
-        if (mx_wide_grad_takes(a)) return launch_mx_wide_grad(a, sizeof(OUT) == 4, stream);
-        go_tile<true, OUT>(a, stream);
-    } else {
-        if (a.rows_vec && a.N % 8 == 0) go_stream_grad<1, true, OUT>(a, stream);
-        else go_stream_grad<1, false, OUT>(a, stream);
-    }
+    if (per_expert > 32 && wide_workgroups(a, 128, a.K) >= 64 && mx_wide_grad_takes(a))
+        return launch_mx_wide_grad(a, per_expert <= 80, sizeof(OUT) == 4, stream);
+    const bool vec = a.rows_vec && a.N % 8 == 0;
+    if (!vec && per_expert > 32) go_tile<true, OUT>(a, stream);
+    else if (!vec) go_stream_grad<1, false, OUT>(a, stream);
+    else if (per_expert >= kTwoTiles) go_stream_grad<2, true, OUT>(a, stream);
+    else go_stream_grad<1, true, OUT>(a, stream);
     return hipGetLastError();
 }
 

@@ -22,7 +22,8 @@ constexpr int kScaleStage = 8 * kScaleRow * 4;
 // 32 >> sn_log2 row tiles by 1 << sn_log2 strips, whose rows and weights they share in that XCD's L2.
 struct WideGrid {
     uint32_t strips, sn_log2, row_tiles, total;
-    __host__ WideGrid(uint64_t row_tiles_most, uint32_t outs) {
+    __host__ WideGrid(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
+        const uint64_t row_tiles_most = a.cap / rows + (a.cap < a.E ? a.cap : a.E);
         strips = (outs + kTile - 1) / kTile;
         sn_log2 = 0;
         while (sn_log2 < 3 && (1u << sn_log2) < strips) ++sn_log2;
@@ -39,12 +40,17 @@ struct WideGrid {
     }
 };
 
-// 16 bytes to each lane's place of the KiB at lds_addr, from its offset to the wavefront's base.  Assembly on purpose: with the compiler's builtin every later LDS read
+// 16 (4) bytes to each lane's place of the KiB (256 bytes) at lds_addr, from its offset to the wavefront's base.  Assembly on purpose: with the compiler's builtin every later LDS read
 // waits for all loads into LDS that are under way, as it cannot tell that they fill another stage.  The waits are those written below, ahead of
 // the barriers.  M0 holds the destination; the compiler has reserved it, so its value is put back.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds_addr) {
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved) : "v"(offset), "s"(base), "s"(lds_addr) : "memory");
+}
+__device__ __forceinline__ void load_word_to_lds(const void* base, uint32_t offset, uint32_t lds_addr) {
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
                  : "=&s"(saved) : "v"(offset), "s"(base), "s"(lds_addr) : "memory");
 }
 template <int N>
@@ -54,14 +60,22 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)
 // round, summed over the outputs.  "Columns" below are those of the result, n0 the tile's first.
 enum Mode { kMxRows, kBf16Rows, kGradRows };
 
+constexpr int kRawScales = kTile * 8;                    // bytes of a superblock's scales
+constexpr int scale_bytes(Mode mode) { return mode == kMxRows ? 0 : 2 * kRawScales + (mode == kGradRows ? 2 * kScaleStage : 0); }
+
+// RT: 32-row groups of a wavefront, 2 for tiles of 256 rows and 1 for 128, whose columns are fetched four steps ahead in as much LDS as two take there.
 // WHOLE: scales are read four at a time
-template <Mode MODE, bool WHOLE, typename OUT>
+template <Mode MODE, int RT, bool WHOLE, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, WideGrid grid) {
     constexpr bool MX = MODE == kMxRows, GRAD = MODE == kGradRows;
-    extern __shared__ __align__(16) uint8_t lds[];           // rows' two stages, weights' two stages, the gradient's scales twice, find_tile's words
+    constexpr uint32_t kRows = 128 * RT;
+    constexpr int kXStages = MX ? 2 : 4 / RT, kXLoads = 2 * RT;      // and a wavefront's loads of a stage
+    constexpr uint32_t kXStage = kRows * 128;
+    // rows' stages, weights' two stages, scales twice (for the gradient as the conversion takes them, then as they come), find_tile's words
+    extern __shared__ __align__(16) uint8_t lds[];
     uint32_t row_tile, strip;
     if (!grid.locate(blockIdx.x, row_tile, strip)) return;
-    const Tile t = find_tile<kThreads>(a, kTile, row_tile, reinterpret_cast<uint32_t*>(lds + 4 * kStage + (GRAD ? 2 * kScaleStage : 0)));
+    const Tile t = find_tile<kThreads>(a, kRows, row_tile, reinterpret_cast<uint32_t*>(lds + 4 * kStage + scale_bytes(MODE)));
     if (t.rows == 0) return;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t wm = wave >> 1, wn = wave & 1, q = lane & 31, h = lane >> 5;
@@ -69,14 +83,15 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     const uint32_t outs = GRAD ? a.K : a.N, supers = GRAD ? (a.N + 255) / 256 : (blocks + 7) / 8;
     const uint32_t lds_base = uint32_t(uintptr_t((__attribute__((address_space(3))) void*)lds));
 
-    // What the lane fetches: four KiB of each operand to a wavefront and stage, rows 8 (4 wave + i) + lane / 8.
+    // What the lane fetches: four KiB of weights to a wavefront and stage, rows 8 (4 wave + i) + lane / 8, and as many or half of rows.
     const uint8_t* const x_base = static_cast<const uint8_t*>(a.rows) + uint64_t(t.first) * a.row_stride;
     const uint8_t* const w_base = a.w + (uint64_t(t.expert) * a.N + (GRAD ? 0 : n0)) * (a.K / 2) + (GRAD ? n0 / 2 : 0);
-    uint32_t x_off[4], w_off[4];                             // of the rows
+    uint32_t x_off[kXLoads], w_off[4];                       // of the rows
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i) x_off[i] = min(8 * (wave * kXLoads + i) + (lane >> 3), t.rows - 1) * uint32_t(a.row_stride);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t row = 8 * (wave * 4 + i) + (lane >> 3);
-        x_off[i] = min(row, t.rows - 1) * uint32_t(a.row_stride);
         w_off[i] = GRAD ? row : min(row, a.N - 1 - n0) * (a.K / 2);
     }
     auto piece_of = [&](int i) __attribute__((always_inline)) { return (lane & 7) ^ ((4 * (i & 1) + (lane >> 4)) & 7); };
@@ -94,12 +109,12 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     // the rows' codes of a superblock, or BF16 columns of its blocks s and 4 + s, into stage `to`
     auto fetch_x = [&](int i, uint32_t super, uint32_t s, uint32_t to) __attribute__((always_inline)) {
         if constexpr (GRAD) {                                // 64 outputs of a superblock's 256
-            load_to_lds(x_base, x_off[i] + min(super * 32 + s * 8 + piece_of(i), a.N / 8 - 1) * 16, lds_base + to * kStage + (wave * 4 + i) * 1024);
+            load_to_lds(x_base, x_off[i] + min(super * 32 + s * 8 + piece_of(i), a.N / 8 - 1) * 16, lds_base + to * kXStage + (wave * kXLoads + i) * 1024);
             return;
         }
         const uint32_t block = min(MX ? piece_of(i) : s + 4 * (piece_of(i) >> 2), blocks - 1 - super * 8);
         load_to_lds(x_base + uint64_t(super) * (MX ? 128 : 512), x_off[i] + block * (MX ? 16 : 64) + (MX ? 0 : (piece_of(i) & 3) * 16),
-                    lds_base + to * kStage + (wave * 4 + i) * 1024);
+                    lds_base + to * kXStage + (wave * kXLoads + i) * 1024);
     };
 
     const row_t ws_at = bytes_at(a.ws, (uint64_t(t.expert) * a.N + n0) * blocks, GRAD ? 0 : min(kTile, a.N - n0) * blocks);
@@ -111,9 +126,9 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
         return four_scales<WHOLE>(xs_at, min((wm + 4 * i) * 32 + q, t.rows - 1) * uint32_t(a.row_scales_stride), super * 8 + 4 * h, blocks);
     };
 
-    f32x16 acc[2][4];
+    f32x16 acc[RT][4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -124,8 +139,26 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) at[ks] = q * 128 + 16 * ((4 * h + ks) ^ ((q >> 1) & 7));
     auto read = [&](uint32_t addr) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(lds + addr); };
-    auto read_x = [&](int i, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + (stage * kStage + wm * 4096) + i * 16384); };
+    auto read_x = [&](int i, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + (stage * kXStage + wm * 4096) + i * 16384); };
     auto read_w = [&](int j, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + ((2 + stage) * kStage + wn * 16384) + j * 4096); };
+
+    // The next superblock's scales as they come: two words of each row, one to a lane
+    auto fetch_words = [&](uint32_t super) __attribute__((always_inline)) {
+        const uint32_t row = tid >> 1, to = lds_base + 4 * kStage + (GRAD ? 2 * kScaleStage : 0) + (super & 1) * kRawScales + wave * 256;
+        if constexpr (GRAD)
+            load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + super * 256) * blocks, min(row, a.N - 1 - super * 256) * blocks + min(n0 / kMxBlock + 4 * (tid & 1), blocks - 4), to);
+        else
+            load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + n0) * blocks, min(row, a.N - 1 - n0) * blocks + min(super * 8 + 4 * (tid & 1), blocks - 4), to);
+    };
+    // Ahead of the barrier of step s the loads that may still be under way: those issued behind the next step's columns, and behind
+    // the next superblock's weights where that is about to begin.  A step issues columns in its last sub-step; steps 0 and 1 issue two loads of
+    // weights each in their first, step 0 a word of scales before those.
+    auto wait_step = [&](auto S, auto MORE) __attribute__((always_inline)) {
+        constexpr int s = decltype(S)::value, words = WHOLE ? 1 : 0;
+        if constexpr (decltype(MORE)::value == 0) wait_loads<RT == 2 ? 0 : s == 0 ? 4 : s == 1 ? 2 : 0>();
+        else if constexpr (RT == 2) wait_loads<s == 0 ? 2 + words : s == 1 ? 2 : 0>();
+        else wait_loads<s == 0 ? 6 + words : s == 3 ? 4 : 8 + words>();
+    };
 
     // ACT: row groups wm, wm + 4 of the tile that have rows
     auto k_loop = [&](auto ACT) __attribute__((always_inline)) {
@@ -221,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             // every fourth one: two bytes of codes of each of eight outputs become the tiles' fragments by a conversion and a permutation to
             // each two numbers.  The scales lie in LDS as the conversion takes them, a block's outputs one after the other.
             uint32_t scales_next = 0;
-            u32x4 fx[2][2], fw[2][4], sc[2];
+            u32x4 fx[2][RT], fw[2][4], sc[2];
             uint32_t raw[8], pair[8][2];
             const uint32_t raw_at = 2 * kStage + h * 4096 + 16 * ((wn * 4 + q / 8) ^ (4 * h)) + 2 * (q & 7);
             const uint32_t sc_at = 4 * kStage + ((wn * 4 + q / 8) * kScaleRow + 32 * h) * 4;
@@ -251,14 +284,21 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                 for (int d = 0; d < 4; ++d)
                     fw[set][c][d] = __builtin_amdgcn_perm(pair[2 * d + 1][c / 2], pair[2 * d][c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
             };
-            fetch_scales(0);
+            auto raw_scales = [&](uint32_t super) __attribute__((always_inline)) {
+                if constexpr (WHOLE) scales_next = *reinterpret_cast<const uint32_t*>(lds + 4 * kStage + 2 * kScaleStage + (super & 1) * kRawScales + tid * 4);
+                else asm volatile("" : "+v"(scales_next));
+            };
+            if constexpr (WHOLE) fetch_words(0);
+            else fetch_scales(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { fetch_w(i, 0); fetch_x(i, 0, 0, 0); }
-            wait_loads<0>();
-            asm volatile("" : "+v"(scales_next));
+            for (int i = 0; i < 4; ++i) fetch_w(i, 0);
+#pragma unroll
+            for (int s = 0; s < kXStages; ++s)
+#pragma unroll
+                for (int i = 0; i < kXLoads; ++i) fetch_x(i, 0, s, s);
+            wait_loads<(kXStages - 1) * kXLoads>();
+            raw_scales(0);                                   // what this wavefront fetched itself
             put_scales(0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) fetch_x(i, 0, 1, 1);
             __syncthreads();
             if constexpr (act > 0) {
                 read_raw(0, 0, 0);
@@ -271,8 +311,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             }
             auto step = [&](auto S, auto MORE, uint32_t super) __attribute__((always_inline)) {
                 constexpr int s = decltype(S)::value;
-                constexpr bool load_w = decltype(MORE)::value != 0, next = load_w || s < 3, load = load_w || s < 2;
-                constexpr uint32_t stage = s & 1;
+                constexpr bool load_w = decltype(MORE)::value != 0, next = load_w || s < 3, load = load_w || s + kXStages < 4;
+                constexpr uint32_t stage = s % kXStages, stage_next = (s + 1) % kXStages;
                 auto sub = [&](auto KS) __attribute__((always_inline)) {
                     constexpr int ks = decltype(KS)::value, set = ks & 1;
                     constexpr bool ahead = act > 0 && (ks < 3 || next);
@@ -296,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                         const int i = n / 4, j = n % 4;
                         if (i < act) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), __builtin_bit_cast(bf16x8, fw[set][j]), acc[i][j], 0, 0, 0);
                         if constexpr (ahead) {
-                            if (n < act) fx[set ^ 1][n] = ks < 3 ? read_x(n, ks + 1, stage) : read_x(n, 0, stage ^ 1);
+                            if (n < act) fx[set ^ 1][n] = ks < 3 ? read_x(n, ks + 1, stage) : read_x(n, 0, stage_next);
                             if (n == 2 || n == 3)
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) convert(4 * (n - 2) + k);
@@ -304,19 +344,21 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                         }
                         // the next superblock's weights, in the first two steps of this one
                         if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
-                        if (ks == 3 && load && (n & 1)) fetch_x(n / 2, super + (s + 2) / 4, (s + 2) % 4, stage);
+                        if (ks == 3 && load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 };
-                if constexpr (s == 0 && load_w) fetch_scales(super + 1);
+                if constexpr (s == 0 && load_w) {
+                    if constexpr (WHOLE) fetch_words(super + 1);
+                    else fetch_scales(super + 1);
+                }
                 sub(Int<0>{});
                 sub(Int<1>{});
                 sub(Int<2>{});
-                if constexpr (s < 2 && load_w) wait_loads<2>();       // all but the two loads of weights that this step issued
-                else wait_loads<0>();
-                if constexpr (s == 2 && load_w) {
-                    asm volatile("" : "+v"(scales_next));
-                    put_scales(super + 1);                            // read behind the next step's barrier
+                wait_step(S, MORE);
+                if constexpr (s == 3 && load_w) {
+                    raw_scales(super + 1);
+                    put_scales(super + 1);
                 }
                 __syncthreads();
                 sub(Int<3>{});
@@ -337,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             // both blocks; its weights are converted in the sub-step before.
             uint32_t scales[4], scales_next[4];
             float sc[4];
-            u32x4 codes[4], fx[2][2];
+            u32x4 codes[4], fx[2][RT];
             bf16x8 fw[2][4];
             auto fetch_scales = [&](uint32_t super) __attribute__((always_inline)) {
 #pragma unroll
@@ -347,16 +389,23 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 #pragma unroll
                 for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(scales_next[j]));
             };
-            fetch_scales(0);
+            auto take_scales = [&](uint32_t super) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { fetch_w(i, 0); fetch_x(i, 0, 0, 0); }
-            wait_loads<0>();
-            scales_arrive();
+                for (int j = 0; j < 4; ++j)
+                    scales[j] = WHOLE ? *reinterpret_cast<const uint32_t*>(lds + 4 * kStage + (super & 1) * kRawScales + (wn * 128 + j * 32 + q) * 8 + 4 * h) : scales_next[j];
+            };
+            if constexpr (WHOLE) fetch_words(0);
+            else fetch_scales(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) scales[j] = scales_next[j];
+            for (int i = 0; i < 4; ++i) fetch_w(i, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fetch_x(i, 0, 1, 1);
+            for (int s = 0; s < kXStages; ++s)
+#pragma unroll
+                for (int i = 0; i < kXLoads; ++i) fetch_x(i, 0, s, s);
+            wait_loads<(kXStages - 1) * kXLoads>();
+            if constexpr (!WHOLE) scales_arrive();
             __syncthreads();
+            take_scales(0);
             if constexpr (act > 0) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) codes[j] = read_w(j, 0, 0);
@@ -371,8 +420,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             // MORE: another superblock follows
             auto step = [&](auto S, auto MORE, uint32_t super) __attribute__((always_inline)) {
                 constexpr int s = decltype(S)::value;
-                constexpr bool load_w = decltype(MORE)::value != 0, next = load_w || s < 3, load = load_w || s < 2;
-                constexpr uint32_t stage = s & 1;
+                constexpr bool load_w = decltype(MORE)::value != 0, next = load_w || s < 3, load = load_w || s + kXStages < 4;
+                constexpr uint32_t stage = s % kXStages, stage_next = (s + 1) % kXStages;
                 auto sub = [&](auto KS) __attribute__((always_inline)) {
                     constexpr int ks = decltype(KS)::value, set = ks & 1;
                     if constexpr (!load_w && act > 0) {      // 0 for blocks past the end, on both sides: a row may hold what is not finite
@@ -392,7 +441,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 #pragma unroll
                             for (int j = 0; j < 4; ++j) codes[j] = read_w(j, (s + 1) % 4, (super + (s == 3)) & 1);
 #pragma unroll
-                            for (int i = 0; i < act; ++i) fx[set ^ 1][i] = read_x(i, 0, stage ^ 1);
+                            for (int i = 0; i < act; ++i) fx[set ^ 1][i] = read_x(i, 0, stage_next);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -406,15 +455,12 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                             // the next superblock's weights, in the first two steps of this one
                             if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
                         } else {
-                            if (load && (n & 1)) fetch_x(n / 2, super + (s + 2) / 4, (s + 2) % 4, stage);
+                            if (load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     if constexpr (ks == 3) {
-                        if constexpr (s == 3) {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) scales[j] = scales_next[j];
-                        }
+                        if constexpr (s == 3 && load_w) take_scales(super + 1);
                         if constexpr (next && act > 0) {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
@@ -424,14 +470,15 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                         }
                     }
                 };
-                if (s == 0 && load_w) fetch_scales(super + 1);
+                if constexpr (s == 0 && load_w) {
+                    if constexpr (WHOLE) fetch_words(super + 1);
+                    else fetch_scales(super + 1);
+                }
                 sub(Int<0>{});
                 sub(Int<1>{});
                 sub(Int<2>{});
-                // all but the two loads of weights that this step issued
-                if (s < 2 && load_w) wait_loads<2>();
-                else wait_loads<0>();
-                if (s == 2) scales_arrive();
+                wait_step(S, MORE);
+                if constexpr (!WHOLE && s == 2 && load_w) scales_arrive();
                 __syncthreads();
                 sub(Int<3>{});
             };
@@ -449,14 +496,14 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
         }
     };
     // (the same for a whole wavefront)
-    if (wm * 32 + 128 < t.rows) k_loop(Int<2>{});
+    if (RT == 2 && wm * 32 + 128 < t.rows) k_loop(Int<RT>{});
     else if (wm * 32 < t.rows) k_loop(Int<1>{});
     else k_loop(Int<0>{});
 
     // Column q of a 32 x 32 result lies in lane q and q + 32, its rows 8 (r / 4) + 4 h + r % 4 in their 16 numbers.  For BF16 neighbouring
     // lanes swap numbers, so that an even lane has two columns of an even row and an odd one of the next: 4-byte stores.
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < RT; ++i) {
         const uint32_t row0 = (wm + 4 * i) * 32 + 4 * h;
         if ((wm + 4 * i) * 32 >= t.rows) break;
         if constexpr (GRAD) {                                // the lane's four columns are those of the four tiles
@@ -513,35 +560,38 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     }
 }
 
-template <Mode MODE, typename OUT>
+template <Mode MODE, int RT, typename OUT>
 void go(const MxProductArgs& a, hipStream_t stream) {
-    const WideGrid grid(a.cap / kTile + (a.cap < a.E ? a.cap : a.E), MODE == kGradRows ? a.K : a.N);
+    const WideGrid grid(a, 128 * RT, MODE == kGradRows ? a.K : a.N);
     const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
     const bool whole = words(a.ws, a.K / kMxBlock) && (MODE != kMxRows || words(a.row_scales, a.row_scales_stride));
     const dim3 wgs(grid.total), threads(kThreads);
-    constexpr uint32_t lds = 4 * kStage + (MODE == kGradRows ? 2 * kScaleStage : 0) + 4 * kTileWords;
-    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, true, OUT>), wgs, threads, lds, stream, a, grid);
-    else hipLaunchKernelGGL((mx_wide_kernel<MODE, false, OUT>), wgs, threads, lds, stream, a, grid);
+    constexpr uint32_t lds = 4 * kStage + scale_bytes(MODE) + 4 * kTileWords;
+    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, true, OUT>), wgs, threads, lds, stream, a, grid);
+    else hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, false, OUT>), wgs, threads, lds, stream, a, grid);
+}
+template <Mode MODE, int RT>
+hipError_t go(const MxProductArgs& a, bool out_f32, hipStream_t stream) {
+    out_f32 ? go<MODE, RT, float>(a, stream) : go<MODE, RT, bf16_t>(a, stream);
+    return hipGetLastError();
 }
 
 bool fits(const MxProductArgs& a, uint32_t outs) {           // places within 31 bits, and a launch of less than 2^31 threads
-    return a.rows_vec && a.row_stride < (1u << 23) && (a.cap / kTile + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(outs) + kTile - 1) / kTile + 8) < (1u << 21);
+    return a.rows_vec && a.row_stride < (1u << 23) && (a.cap / 128 + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(outs) + kTile - 1) / kTile + 8) < (1u << 21);
 }
 
 }  // namespace
 
 bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) { return fits(a, a.N) && (!mx_rows || a.row_scales_stride < (1u << 22)); }
-hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream) {
-    if (mx_rows) out_f32 ? go<kMxRows, float>(a, stream) : go<kMxRows, bf16_t>(a, stream);
-    else out_f32 ? go<kBf16Rows, float>(a, stream) : go<kBf16Rows, bf16_t>(a, stream);
-    return hipGetLastError();
+hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool half, bool out_f32, hipStream_t stream) {
+    if (mx_rows) return go<kMxRows, 2>(a, out_f32, stream);
+    return half ? go<kBf16Rows, 1>(a, out_f32, stream) : go<kBf16Rows, 2>(a, out_f32, stream);
 }
 
 // (d_out's rows are whole 16-byte pieces: of one that reaches past a row's end the rest would be multiplied)
 bool mx_wide_grad_takes(const MxProductArgs& a) { return fits(a, a.K) && a.N % 8 == 0; }
-hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream) {
-    out_f32 ? go<kGradRows, float>(a, stream) : go<kGradRows, bf16_t>(a, stream);
-    return hipGetLastError();
+hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool half, bool out_f32, hipStream_t stream) {
+    return half ? go<kGradRows, 1>(a, out_f32, stream) : go<kGradRows, 2>(a, out_f32, stream);
 }
 
 }  // namespace fluxmoe
