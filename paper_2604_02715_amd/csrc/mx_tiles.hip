@@ -61,7 +61,7 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)
 enum Mode { kMxRows, kBf16Rows, kGradRows };
 
 constexpr int kRawScales = kTile * 8;                    // bytes of a superblock's scales
-constexpr int scale_bytes(Mode mode) { return mode == kMxRows ? 0 : 2 * kRawScales + (mode == kGradRows ? 2 * kScaleStage : 0); }
+constexpr int scale_bytes(Mode mode) { return mode == kMxRows ? 4 * kRawScales : 2 * kRawScales + (mode == kGradRows ? 2 * kScaleStage : 0); }
 
 // RT: 32-row groups of a wavefront, 2 for tiles of 256 rows and 1 for 128, whose columns are fetched four steps ahead in as much LDS as two take there.
 // WHOLE: scales are read four at a time
@@ -71,7 +71,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     constexpr uint32_t kRows = 128 * RT;
     constexpr int kXStages = MX ? 2 : 4 / RT, kXLoads = 2 * RT;      // and a wavefront's loads of a stage
     constexpr uint32_t kXStage = kRows * 128;
-    // rows' stages, weights' two stages, scales twice (for the gradient as the conversion takes them, then as they come), find_tile's words
+    // rows' stages, weights' two stages, scales twice (for the gradient as the conversion takes them, then as they come; for rows in 4 bits the
+    // weights', then the rows'), find_tile's words
     extern __shared__ __align__(16) uint8_t lds[];
     uint32_t row_tile, strip;
     if (!grid.locate(blockIdx.x, row_tile, strip)) return;
@@ -142,9 +143,13 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     auto read_x = [&](int i, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + (stage * kXStage + wm * 4096) + i * 16384); };
     auto read_w = [&](int j, int ks, uint32_t stage) __attribute__((always_inline)) { return read(at[ks] + ((2 + stage) * kStage + wn * 16384) + j * 4096); };
 
-    // The next superblock's scales as they come: two words of each row, one to a lane
+    // The next superblock's scales as they come: two words of each row, one to a lane.  (Fetched by the lanes that multiply by them, a word from
+    // each of 32 rows at a time, they were a third of a step: 16382 rows in 4 bits of 14336 columns, 4096 outputs 822 us, through LDS 572.)
     auto fetch_words = [&](uint32_t super) __attribute__((always_inline)) {
         const uint32_t row = tid >> 1, to = lds_base + 4 * kStage + (GRAD ? 2 * kScaleStage : 0) + (super & 1) * kRawScales + wave * 256;
+        if constexpr (MX)
+            load_word_to_lds(a.row_scales + uint64_t(t.first) * a.row_scales_stride, min(row, t.rows - 1) * uint32_t(a.row_scales_stride) + min(super * 8 + 4 * (tid & 1), blocks - 4),
+                             to + 2 * kRawScales);
         if constexpr (GRAD)
             load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + super * 256) * blocks, min(row, a.N - 1 - super * 256) * blocks + min(n0 / kMxBlock + 4 * (tid & 1), blocks - 4), to);
         else
@@ -174,6 +179,13 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 #pragma unroll
                 for (int i = 0; i < act; ++i) xs_next[i] = x_scales(i, super);
             };
+            auto read_scales = [&](uint32_t super) __attribute__((always_inline)) {
+                const uint8_t* from = lds + 4 * kStage + (super & 1) * kRawScales + 4 * h;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) ws_next[j] = *reinterpret_cast<const uint32_t*>(from + (wn * 128 + j * 32 + q) * 8);
+#pragma unroll
+                for (int i = 0; i < act; ++i) xs_next[i] = *reinterpret_cast<const uint32_t*>(from + 2 * kRawScales + ((wm + 4 * i) * 32 + q) * 8);
+            };
             auto scales_arrive = [&]() __attribute__((always_inline)) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) { asm volatile("" : "+v"(ws_next[j])); }
@@ -195,6 +207,13 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                 constexpr int ks = decltype(KS)::value, set = ks & 1;
                 constexpr bool next = decltype(NEXT)::value != 0, load = decltype(LOAD)::value != 0;
                 if constexpr (!next && act > 0) {           // 0 for blocks past the end; the rows' codes are finite whatever they are
+                    if constexpr (WHOLE && ks == 0) {        // and so are scales
+                        const bool in = super * 8 + 4 * h < blocks;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) ws[j] = in ? ws[j] : 0;
+#pragma unroll
+                        for (int i = 0; i < act; ++i) xs[i] = in ? xs[i] : 0;
+                    }
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -212,6 +231,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                         if (n < 6) read_item(n, stage, ks + 1, set ^ 1);
                     } else {
                         if (next && n < 6) read_item(n, stage ^ 1, 0, set ^ 1);
+                        if (WHOLE && next && n == 6) read_scales(super + 1);
+                        if (WHOLE && load && n == 0) fetch_words(super + 2);
                         if (load) {
                             if (n & 1) fetch_w(n / 2, super + 2);
                             else fetch_x(n / 2, super + 2, 0, stage);
@@ -222,27 +243,35 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             };
             auto step = [&](auto NEXT, auto LOAD, uint32_t super) __attribute__((always_inline)) {
                 const uint32_t stage = super & 1;
-                if constexpr (decltype(NEXT)::value != 0) fetch_scales(super + 1);
+                if constexpr (!WHOLE && decltype(NEXT)::value != 0) fetch_scales(super + 1);
                 sub(Int<0>{}, NEXT, LOAD, stage, super);
                 sub(Int<1>{}, NEXT, LOAD, stage, super);
                 sub(Int<2>{}, NEXT, LOAD, stage, super);
                 wait_loads<0>();
-                scales_arrive();
+                if constexpr (!WHOLE) scales_arrive();
                 __syncthreads();
                 sub(Int<3>{}, NEXT, LOAD, stage, super);
                 take_scales();
             };
-            fetch_scales(0);
+            if constexpr (WHOLE) fetch_words(0);
+            else fetch_scales(0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) { fetch_w(i, 0); fetch_x(i, 0, 0, 0); }
-            wait_loads<0>();
-            scales_arrive();
-            take_scales();
+            if constexpr (!WHOLE) {
+                wait_loads<0>();
+                scales_arrive();
+            }
             if (supers > 1) {
+                if constexpr (WHOLE) fetch_words(1);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) { fetch_w(i, 1); fetch_x(i, 1, 0, 1); }
+                wait_loads<8 + (WHOLE ? 2 : 0)>();
+            } else {
+                wait_loads<0>();
             }
             __syncthreads();
+            if constexpr (WHOLE) read_scales(0);
+            take_scales();
 #pragma unroll
             for (int n = 0; n < 6; ++n) read_item(n, 0, 0, 0);
             uint32_t super = 0;
