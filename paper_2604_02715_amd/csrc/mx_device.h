@@ -15,23 +15,34 @@ struct Tile {
     uint32_t expert, first, rows;            // rows 0: no such tile
 };
 
-// Rows of expert e that lie within the matrix, whatever offsets and counts hold.
-__device__ __forceinline__ uint32_t rows_of(const MxProductArgs& a, uint32_t e) {
+// Rows of expert e that lie within the matrix, whatever offsets and counts hold, and the first of them.
+__device__ __forceinline__ uint32_t rows_of(const MxProductArgs& a, uint32_t e, uint32_t& first) {
     const int32_t c = a.counts[e], o = a.offsets[e];
-    if (c <= 0 || o < 0 || uint32_t(o) >= a.cap) return 0;
-    return min(uint32_t(c), a.cap - uint32_t(o));
+    first = uint32_t(o);
+    return c <= 0 || o < 0 || uint32_t(o) >= a.cap ? 0 : min(uint32_t(c), a.cap - uint32_t(o));
 }
 
-// Tile number `wanted` of the experts' groups in their order, `size` rows to a tile.  All threads of the workgroup; a thread
-// adds up neighbouring experts.  s: kTileWords of LDS.
+// Tile number `wanted` of the experts' groups in their order, `size` rows to a tile; rows 0 where there are no more.  All threads of the
+// workgroup; a thread adds up neighbouring experts and keeps what it read of up to four.  s: kTileWords of LDS.
 constexpr uint32_t kTileWords = 16;
 template <uint32_t THREADS>
 __device__ __forceinline__ Tile find_tile(const MxProductArgs& a, uint32_t size, uint32_t wanted, uint32_t* s) {
+    constexpr uint32_t kFound = THREADS / 64, kKept = 4;
+    static_assert(kFound + 3 <= kTileWords, "wavefronts' sums and the tile");
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t per = (a.E + THREADS - 1) / THREADS, from = min(tid * per, a.E), to = min(from + per, a.E);
-    static_assert(THREADS / 64 + 3 <= kTileWords, "wavefronts' sums and the tile");
-    uint32_t mine = 0;
-    for (uint32_t e = from; e < to; ++e) mine += (rows_of(a, e) + size - 1) / size;
+    uint32_t rows[kKept], first[kKept], mine = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kKept; ++i) {
+        rows[i] = first[i] = 0;
+        if (from + i < to) rows[i] = rows_of(a, from + i, first[i]);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kKept; ++i) mine += (rows[i] + size - 1) / size;
+    for (uint32_t e = from + kKept; e < to; ++e) {
+        uint32_t at;
+        mine += (rows_of(a, e, at) + size - 1) / size;
+    }
     uint32_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -40,29 +51,48 @@ __device__ __forceinline__ Tile find_tile(const MxProductArgs& a, uint32_t size,
     }
     __syncthreads();                                     // the last tile's readers are done with s
     if (lane == 63) s[wave] = upto;
-    if (tid == 0) s[THREADS / 64 + 2] = 0;
+    if (tid == 0) s[kFound + 2] = 0;
     __syncthreads();
     for (uint32_t w = 0; w < wave; ++w) upto += s[w];
     uint32_t before = upto - mine;
     if (wanted >= before && wanted < upto) {
-        for (uint32_t e = from; e < to; ++e) {
-            const uint32_t rows = rows_of(a, e), tiles = (rows + size - 1) / size;
-            if (wanted < before + tiles) {
-                const uint32_t at = (wanted - before) * size;
-                s[THREADS / 64] = e;
-                s[THREADS / 64 + 1] = uint32_t(a.offsets[e]) + at;
-                s[THREADS / 64 + 2] = min(size, rows - at);
-                break;
+        auto found = [&](uint32_t e, uint32_t n, uint32_t at) __attribute__((always_inline)) {
+            const uint32_t tiles = (n + size - 1) / size, skip = (wanted - before) * size;
+            const bool here = wanted >= before && wanted < before + tiles;
+            if (here) {
+                s[kFound] = e;
+                s[kFound + 1] = at + skip;
+                s[kFound + 2] = min(size, n - skip);
             }
             before += tiles;
+            return here;
+        };
+#pragma unroll
+        for (uint32_t i = 0; i < kKept; ++i) found(from + i, rows[i], first[i]);
+        for (uint32_t e = from + kKept; e < to; ++e) {
+            uint32_t at;
+            const uint32_t n = rows_of(a, e, at);
+            if (found(e, n, at)) break;
         }
     }
     __syncthreads();
     Tile t;
-    t.expert = __builtin_amdgcn_readfirstlane(s[THREADS / 64]);
-    t.first = __builtin_amdgcn_readfirstlane(s[THREADS / 64 + 1]);
-    t.rows = __builtin_amdgcn_readfirstlane(s[THREADS / 64 + 2]);
+    t.expert = __builtin_amdgcn_readfirstlane(s[kFound]);
+    t.first = __builtin_amdgcn_readfirstlane(s[kFound + 1]);
+    t.rows = __builtin_amdgcn_readfirstlane(s[kFound + 2]);
     return t;
+}
+
+// Item number `item` of a launch over tiles of `strips` strips each: (tile, strip).  Nearly always within 32 bits, where a division is a
+// tenth as long.
+struct Item {
+    uint32_t tile, strip;
+};
+__device__ __forceinline__ Item item_at(uint64_t item, uint32_t strips) {
+    Item i;
+    i.tile = item >> 32 ? uint32_t(item / strips) : uint32_t(item) / strips;
+    i.strip = uint32_t(item - uint64_t(i.tile) * strips);
+    return i;
 }
 
 // `records` bytes from `base` on, by offset: reads past them give 0

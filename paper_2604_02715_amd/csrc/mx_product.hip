@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
     const uint32_t blocks = a.K / kMxBlock, supers = (blocks + 15) / 16;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
+        const auto [tile_at, strip] = item_at(item, strips);
         const Tile t = find_tile<kThreads>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;                         // nor are there any behind it
         const uint32_t n0 = strip * kWidth + (KS == 1 ? wave * (16 * NI) : 0), outs = n0 < a.N ? min(a.N - n0, uint32_t(16 * NI)) : 0;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
     const uint32_t blocks = a.K / kMxBlock, steps = (blocks + 7) / 8;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
+        const auto [tile_at, strip] = item_at(item, strips);
         const Tile t = find_tile<kThreads>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;
         const uint32_t n0 = (strip * 4 + wave) * (16 * NI), outs = n0 < a.N ? min(a.N - n0, uint32_t(16 * NI)) : 0;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArg
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
     const uint32_t blocks = a.K / kMxBlock, chunks = (a.N + 31) / 32;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
+        const auto [tile_at, strip] = item_at(item, strips);
         const Tile t = find_tile<64 * WAVES>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;
         const uint32_t k0 = strip * 256, column = k0 + r * 16;
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void mx_tile_kernel(MxProductArgs a, uint
     const uint32_t sum = GRAD ? a.N : a.K, outs = GRAD ? a.K : a.N, blocks = a.K / kMxBlock;
     const uint32_t m_wave = (wave >> 1) * 64, n_wave = (wave & 1) * 64;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t tile_at = uint32_t(item / strips), strip = uint32_t(item - uint64_t(tile_at) * strips);
+        const auto [tile_at, strip] = item_at(item, strips);
         const Tile t = find_tile<kThreads>(a, BM, tile_at, s_tile);
         if (t.rows == 0) return;
         const uint32_t n0 = strip * BN;

@@ -19,22 +19,18 @@ from .moe_block import _TYPES, _fail, _matrix, _place, _ptr, _sptr, _too_large, 
 BLOCK = 32                      # columns that share a scale
 
 
-def _as_rows(t, name):
-    """A matrix as it is; more dimensions without gaps (all experts' weights) as one of all their rows."""
-    if t.dim() < 2:
-        _fail("%s must be [rows][columns]" % name)
-    if t.dim() == 2:
-        return t
-    if not t.is_contiguous():
-        _fail("%s of more than two dimensions must be contiguous" % name)
+def _as_rows(t, name, rows_of):
+    """All experts' rows as those of one matrix: more than two dimensions, without gaps"""
+    if t.dim() < 2 or not t.is_contiguous():
+        _fail("%s must be [rows][columns], or contiguous with more dimensions" % name)
+    if t.shape[:-1] != rows_of.shape[:-1]:
+        _fail("%s must have the rows of the other tensors, got %s" % (name, list(t.shape)))
     return t.view(-1, t.shape[-1])
 
 
 def _mx_rows(x, x_name, codes, scales):
-    for t, name in ((codes, "codes"), (scales, "scales")):
-        if t.shape[:-1] != x.shape[:-1]:
-            _fail("%s must have the rows of %s, got %s" % (name, x_name, list(t.shape)))
-    x, codes, scales = _as_rows(x, x_name), _as_rows(codes, "codes"), _as_rows(scales, "scales")
+    if not x.dim() == codes.dim() == scales.dim() == 2:
+        x, codes, scales = _as_rows(x, x_name, codes), _as_rows(codes, "codes", scales), _as_rows(scales, "scales", x)
     device = _place(x, x_name)
     rows, columns = x.shape
     if columns % BLOCK:
