@@ -94,10 +94,7 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
                         xv[m][i] = u32x4{0, 0, 0, 0};
                         if (have[m] && block + 4 * i < blocks) {
                             if constexpr (VEC) xv[m][i] = *reinterpret_cast<const u32x4*>(src[m] + (block + 4 * i) * 16);
-                            else {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) xv[m][i][j / 4] |= uint32_t(uint8_t(src[m][(block + 4 * i) * 16 + j])) << (8 * (j & 3));
-                            }
+                            else __builtin_memcpy(&xv[m][i], src[m] + (block + 4 * i) * 16, 16);
                         }
                     }
                 }
@@ -128,11 +125,7 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
                             xv[m][j] = u32x4{0, 0, 0, 0};
                             if (have[m] && block + 4 * i < blocks) {
                                 if constexpr (VEC) xv[m][j] = *reinterpret_cast<const u32x4*>(src[m] + (block + 4 * i) * 64 + j * 16);
-                                else {
-                                    const uint16_t* p = reinterpret_cast<const uint16_t*>(src[m]) + (block + 4 * i) * 32 + j * 8;
-#pragma unroll
-                                    for (int c = 0; c < 8; ++c) xv[m][j][c / 2] |= uint32_t(p[c]) << (16 * (c & 1));
-                                }
+                                else __builtin_memcpy(&xv[m][j], src[m] + (block + 4 * i) * 64 + j * 16, 16);
                             }
                         }
 #pragma unroll
@@ -345,9 +338,13 @@ __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArg
                 if (m * 16 + r < t.rows) {
                     if (VEC && n < a.N) x[m] = *reinterpret_cast<const u32x4*>(p);
                     if constexpr (!VEC) {
+                        if (n + 8 <= a.N) {
+                            __builtin_memcpy(&x[m], p, 16);
+                        } else {
 #pragma unroll
-                        for (uint32_t j = 0; j < 8; ++j)
-                            if (n + j < a.N) x[m][j / 2] |= uint32_t(p[j]) << (16 * (j & 1));
+                            for (uint32_t j = 0; j < 8; ++j)
+                                if (n + j < a.N) x[m][j / 2] |= uint32_t(p[j]) << (16 * (j & 1));
+                        }
                     }
                 }
             }
@@ -400,121 +397,6 @@ __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArg
     }
 }
 
-// ---------------------------------------------------------------- many rows: tiles in LDS
-// Both operands lie in LDS as BF16 rows of 64 summed columns (128 bytes), the weights converted on their way there; a 16-byte
-// piece lies at its number xor swizzle(row), which spreads the rows' pieces over the banks.  GRAD sums over the outputs: the
-// weights are turned round on their way, eight outputs by four columns to a thread.
-__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t piece) { return row * 8 + (piece ^ ((row ^ (row >> 3)) & 7)); }
-
-template <bool GRAD, typename OUT>
-__global__ __launch_bounds__(kThreads) void mx_tile_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
-    constexpr uint32_t BM = 128, BN = 128;
-    __shared__ uint32_t s_tile[kTileWords];
-    __shared__ u32x4 s_x[BM * 8], s_w[BN * 8];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t sum = GRAD ? a.N : a.K, outs = GRAD ? a.K : a.N, blocks = a.K / kMxBlock;
-    const uint32_t m_wave = (wave >> 1) * 64, n_wave = (wave & 1) * 64;
-    for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const auto [tile_at, strip] = item_at(item, strips);
-        const Tile t = find_tile<kThreads>(a, BM, tile_at, s_tile);
-        if (t.rows == 0) return;
-        const uint32_t n0 = strip * BN;
-        const char* x = static_cast<const char*>(a.rows) + uint64_t(t.first) * a.row_stride;
-        const uint8_t* w = a.w + uint64_t(t.expert) * a.N * (a.K / 2);
-        const uint8_t* ws = a.ws + uint64_t(t.expert) * a.N * blocks;
-        f32x16 acc[2][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[i / 2][i % 2][j] = 0.0f;
-
-        for (uint32_t k0 = 0; k0 < sum; k0 += 64) {
-            u32x4 xv[4], wv[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t at = tid + i * kThreads, row = at / 8, k = k0 + (at & 7) * 8;
-                xv[i] = u32x4{0, 0, 0, 0};
-                if (row < t.rows && k < sum) {
-                    const uint16_t* p = reinterpret_cast<const uint16_t*>(x + uint64_t(row) * a.row_stride) + k;
-                    if (a.rows_vec && k + 8 <= sum) xv[i] = *reinterpret_cast<const u32x4*>(p);
-                    else {
-#pragma unroll
-                        for (uint32_t j = 0; j < 8; ++j)
-                            if (k + j < sum) xv[i][j / 2] |= uint32_t(p[j]) << (16 * (j & 1));
-                    }
-                }
-            }
-            if constexpr (GRAD) {
-                const uint32_t ng = tid >> 5, k4 = n0 + (tid & 31) * 4;
-                uint32_t v[8][2];
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) {
-                    const uint64_t n = k0 + ng * 8 + j;
-                    uint32_t codes = 0, s = 0;
-                    if (n < sum && k4 < outs) {
-                        codes = *reinterpret_cast<const uint16_t*>(w + n * (a.K / 2) + k4 / 2);
-                        s = ws[n * blocks + k4 / kMxBlock];
-                    }
-                    v[j][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale_operand(s), 0));
-                    v[j][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale_operand(s), 1));
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const uint32_t lo = v[2 * d][c / 2], hi = v[2 * d + 1][c / 2];
-                        wv[c][d] = (c & 1) ? (lo >> 16) | (hi & 0xFFFF0000u) : (lo & 0xFFFFu) | (hi << 16);
-                    }
-            } else {
-                const uint32_t n = n0 + tid / 2, block = k0 / kMxBlock + (tid & 1);
-                u32x4 codes = {0, 0, 0, 0};
-                uint32_t s = 0;
-                if (n < outs && block < blocks) {
-                    codes = *reinterpret_cast<const u32x4*>(w + uint64_t(n) * (a.K / 2) + block * 16);
-                    s = ws[uint64_t(n) * blocks + block];
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) wv[j] = __builtin_bit_cast(u32x4, codes_bf16(codes[j], scale_operand(s)));
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t at = tid + i * kThreads;
-                s_x[piece_at(at / 8, at & 7)] = xv[i];
-                if constexpr (GRAD) s_w[piece_at((tid & 31) * 4 + i, tid >> 5)] = wv[i];
-                else s_w[piece_at(tid / 2, (tid & 1) * 4 + i)] = wv[i];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                bf16x8 xf[2], wf[2];
-                const uint32_t piece = ks * 2 + lane / 32;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    xf[i] = __builtin_bit_cast(bf16x8, s_x[piece_at(m_wave + i * 32 + (lane & 31), piece)]);
-                    wf[i] = __builtin_bit_cast(bf16x8, s_w[piece_at(n_wave + i * 32 + (lane & 31), piece)]);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[i], wf[j], acc[i][j], 0, 0, 0);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t n = n0 + n_wave + j * 32 + (lane & 31);
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const uint32_t row = m_wave + i * 32 + (c / 4) * 8 + (lane / 32) * 4 + c % 4;
-                    if (row < t.rows && n < outs)
-                        from_float(reinterpret_cast<OUT*>(static_cast<char*>(a.out) + uint64_t(t.first + row) * a.out_stride) + n, acc[i][j][c]);
-                }
-            }
-    }
-}
-
 // Tiles that the groups can have: full ones and one unfinished one for each expert that has rows.
 uint64_t most_tiles(const MxProductArgs& a, uint32_t size) { return a.cap / size + (a.cap < a.E ? a.cap : a.E); }
 
@@ -553,12 +435,6 @@ void go_stream_grad(const MxProductArgs& a, hipStream_t stream) {
     else
         hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 4, VEC, OUT>), dim3(p.grid), dim3(256), 0, stream, a, p.strips, p.items);
 }
-template <bool GRAD, typename OUT>
-void go_tile(const MxProductArgs& a, hipStream_t stream) {
-    const Plan p(a, 128, GRAD ? a.K : a.N, 128);
-    hipLaunchKernelGGL((mx_tile_kernel<GRAD, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
-}
-
 template <int MI, int NI, bool MX, typename OUT>
 void go_strip(const MxProductArgs& a, bool whole, hipStream_t stream) {
     const Plan p(a, 16 * MI, a.N, 64 * NI);
@@ -608,8 +484,7 @@ hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     } else {
         if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 192 && mx_wide_takes(a, false))
             return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 256, sizeof(OUT) == 4, stream);
-        if (!a.rows_vec && per_expert > 32) go_tile<false, OUT>(a, stream);
-        else if (!a.rows_vec) go_stream<1, 4, 4, false, false, OUT>(a, stream);
+        if (!a.rows_vec) go_stream<2, 4, 4, false, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, false, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, false, OUT>(a, stream);
         else pick_stream<1, false, OUT>(a, stream);
@@ -623,10 +498,8 @@ hipError_t product_grad(const MxProductArgs& a, hipStream_t stream) {
     if (per_expert > 32 && wide_workgroups(a, 128, a.K) >= 64 && mx_wide_grad_takes(a))
         return launch_mx_wide_grad(a, per_expert <= 80, sizeof(OUT) == 4, stream);
     const bool vec = a.rows_vec && a.N % 8 == 0;
-    if (!vec && per_expert > 32) go_tile<true, OUT>(a, stream);
-    else if (!vec) go_stream_grad<1, false, OUT>(a, stream);
-    else if (per_expert >= kTwoTiles) go_stream_grad<2, true, OUT>(a, stream);
-    else go_stream_grad<1, true, OUT>(a, stream);
+    if (per_expert >= kTwoTiles) vec ? go_stream_grad<2, true, OUT>(a, stream) : go_stream_grad<2, false, OUT>(a, stream);
+    else vec ? go_stream_grad<1, true, OUT>(a, stream) : go_stream_grad<1, false, OUT>(a, stream);
     return hipGetLastError();
 }
 

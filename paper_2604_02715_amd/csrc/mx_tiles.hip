@@ -64,10 +64,11 @@ constexpr int kRawScales = kTile * 8;                    // bytes of a superbloc
 constexpr int scale_bytes(Mode mode) { return mode == kMxRows ? 4 * kRawScales : 2 * kRawScales + (mode == kGradRows ? 2 * kScaleStage : 0); }
 
 // RT: 32-row groups of a wavefront, 2 for tiles of 256 rows and 1 for 128, whose columns are fetched four steps ahead in as much LDS as two take there.
-// WHOLE: scales are read four at a time
-template <Mode MODE, int RT, bool WHOLE, typename OUT>
+// WHOLE: scales are read four at a time.  VEC: the rows are whole 16-byte pieces at 16-byte addresses; others come through registers.
+template <Mode MODE, int RT, bool WHOLE, bool VEC, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, WideGrid grid) {
     constexpr bool MX = MODE == kMxRows, GRAD = MODE == kGradRows;
+    static_assert(VEC || (!MX && !WHOLE), "BF16 rows at any address, scales too");
     constexpr uint32_t kRows = 128 * RT;
     constexpr int kXStages = MX ? 2 : 4 / RT, kXLoads = 2 * RT;      // and a wavefront's loads of a stage
     constexpr uint32_t kXStage = kRows * 128;
@@ -118,6 +119,25 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                     lds_base + to * kXStage + (wave * kXLoads + i) * 1024);
     };
 
+    // (not VEC) The same pieces into registers, to be put where the loads into LDS would put them in the next step.  0 past a row's end: a piece
+    // that reaches beyond it is the row's last eight numbers, moved.  No branches: between matrix instructions they would be moved behind them.
+    u32x4 held[VEC ? 1 : kXLoads];
+    auto hold_x = [&](int i, uint32_t super, uint32_t s) __attribute__((always_inline)) {
+        const uint32_t sum = GRAD ? a.N : a.K;
+        const uint32_t column = GRAD ? super * 256 + s * 64 + piece_of(i) * 8 : (super * 8 + s + 4 * (piece_of(i) >> 2)) * 32 + (piece_of(i) & 3) * 8;
+        const uint32_t from = min(column, sum - 8), beyond = min(column - from, 8u);
+        uint64_t v[2];
+        __builtin_memcpy(v, x_base + x_off[i] + from * 2, 16);
+        const uint64_t low = beyond >= 4 ? v[1] : v[0], high = beyond >= 4 ? 0 : v[1];
+        const uint32_t by = 16 * (beyond & 3);
+        const uint64_t a0 = beyond == 8 ? 0 : (low >> by) | ((high << 1) << (63 - by)), a1 = high >> by;
+        held[i] = u32x4{uint32_t(a0), uint32_t(a0 >> 32), uint32_t(a1), uint32_t(a1 >> 32)};
+    };
+    auto put_x = [&](uint32_t to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i) *reinterpret_cast<u32x4*>(lds + to * kXStage + (wave * kXLoads + i) * 1024 + lane * 16) = held[i];
+    };
+
     const row_t ws_at = bytes_at(a.ws, (uint64_t(t.expert) * a.N + n0) * blocks, GRAD ? 0 : min(kTile, a.N - n0) * blocks);
     const row_t xs_at = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
     auto w_scales = [&](int j, uint32_t super) __attribute__((always_inline)) {
@@ -155,14 +175,42 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
         else
             load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + n0) * blocks, min(row, a.N - 1 - n0) * blocks + min(super * 8 + 4 * (tid & 1), blocks - 4), to);
     };
+    // the columns of a tile's first steps
+    auto first_rows = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < kXStages; ++s) {
+#pragma unroll
+            for (int i = 0; i < kXLoads; ++i) {
+                if constexpr (VEC) fetch_x(i, 0, s, s);
+                else hold_x(i, 0, s);
+            }
+            if constexpr (!VEC) put_x(s);
+        }
+        wait_loads<VEC ? (kXStages - 1) * kXLoads : 0>();
+    };
     // Ahead of the barrier of step s the loads that may still be under way: those issued behind the next step's columns, and behind
     // the next superblock's weights where that is about to begin.  A step issues columns in its last sub-step; steps 0 and 1 issue two loads of
     // weights each in their first, step 0 a word of scales before those.
     auto wait_step = [&](auto S, auto MORE) __attribute__((always_inline)) {
         constexpr int s = decltype(S)::value, words = WHOLE ? 1 : 0;
-        if constexpr (decltype(MORE)::value == 0) wait_loads<RT == 2 ? 0 : s == 0 ? 4 : s == 1 ? 2 : 0>();
+        if constexpr (!VEC) wait_loads<0>();
+        else if constexpr (decltype(MORE)::value == 0) wait_loads<RT == 2 ? 0 : s == 0 ? 4 : s == 1 ? 2 : 0>();
         else if constexpr (RT == 2) wait_loads<s == 0 ? 2 + words : s == 1 ? 2 : 0>();
         else wait_loads<s == 0 ? 6 + words : s == 3 ? 4 : 8 + words>();
+    };
+
+    // (not VEC) Behind step s's barrier its columns' stage is free: what is to lie there is fetched, and put there ahead of the next barrier.
+    auto take_up = [&](auto S, auto MORE, uint32_t super) __attribute__((always_inline)) {
+        constexpr int s = decltype(S)::value;
+        if constexpr (!VEC && (decltype(MORE)::value != 0 || s + kXStages < 4)) {
+#pragma unroll
+            for (int i = 0; i < kXLoads; ++i) hold_x(i, super + (s + kXStages) / 4, (s + kXStages) % 4);
+        }
+    };
+    auto hand_over = [&](auto S, auto MORE) __attribute__((always_inline)) {
+        constexpr int s = decltype(S)::value;
+        if constexpr (!VEC && s == 0) put_x(3 % kXStages);       // of the last superblock's step 3, or once more of the tile's first steps
+        else if constexpr (!VEC && (decltype(MORE)::value != 0 || s - 1 + kXStages < 4)) put_x((s - 1) % kXStages);
     };
 
     // ACT: row groups wm, wm + 4 of the tile that have rows
@@ -321,11 +369,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             else fetch_scales(0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) fetch_w(i, 0);
-#pragma unroll
-            for (int s = 0; s < kXStages; ++s)
-#pragma unroll
-                for (int i = 0; i < kXLoads; ++i) fetch_x(i, 0, s, s);
-            wait_loads<(kXStages - 1) * kXLoads>();
+            first_rows();
             raw_scales(0);                                   // what this wavefront fetched itself
             put_scales(0);
             __syncthreads();
@@ -373,7 +417,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                         }
                         // the next superblock's weights, in the first two steps of this one
                         if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
-                        if (ks == 3 && load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
+                        if (VEC && ks == 3 && load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 };
@@ -384,12 +428,14 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                 sub(Int<0>{});
                 sub(Int<1>{});
                 sub(Int<2>{});
+                hand_over(S, MORE);
                 wait_step(S, MORE);
                 if constexpr (s == 3 && load_w) {
                     raw_scales(super + 1);
                     put_scales(super + 1);
                 }
                 __syncthreads();
+                take_up(S, MORE, super);
                 sub(Int<3>{});
             };
             uint32_t super = 0;
@@ -427,11 +473,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             else fetch_scales(0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) fetch_w(i, 0);
-#pragma unroll
-            for (int s = 0; s < kXStages; ++s)
-#pragma unroll
-                for (int i = 0; i < kXLoads; ++i) fetch_x(i, 0, s, s);
-            wait_loads<(kXStages - 1) * kXLoads>();
+            first_rows();
             if constexpr (!WHOLE) scales_arrive();
             __syncthreads();
             take_scales(0);
@@ -484,7 +526,7 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                             // the next superblock's weights, in the first two steps of this one
                             if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
                         } else {
-                            if (load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
+                            if (VEC && load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -506,9 +548,11 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                 sub(Int<0>{});
                 sub(Int<1>{});
                 sub(Int<2>{});
+                hand_over(S, MORE);
                 wait_step(S, MORE);
                 if constexpr (!WHOLE && s == 2 && load_w) scales_arrive();
                 __syncthreads();
+                take_up(S, MORE, super);
                 sub(Int<3>{});
             };
             uint32_t super = 0;
@@ -590,37 +634,44 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 }
 
 template <Mode MODE, int RT, typename OUT>
-void go(const MxProductArgs& a, hipStream_t stream) {
+void go(const MxProductArgs& a, bool vec, hipStream_t stream) {
     const WideGrid grid(a, 128 * RT, MODE == kGradRows ? a.K : a.N);
     const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
     const bool whole = words(a.ws, a.K / kMxBlock) && (MODE != kMxRows || words(a.row_scales, a.row_scales_stride));
     const dim3 wgs(grid.total), threads(kThreads);
     constexpr uint32_t lds = 4 * kStage + scale_bytes(MODE) + 4 * kTileWords;
-    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, true, OUT>), wgs, threads, lds, stream, a, grid);
-    else hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, false, OUT>), wgs, threads, lds, stream, a, grid);
+    if constexpr (MODE == kGradRows || (MODE == kBf16Rows && RT == 1)) {
+        if (!vec) {
+            hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, false, false, OUT>), wgs, threads, lds, stream, a, grid);
+            return;
+        }
+    }
+    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, true, true, OUT>), wgs, threads, lds, stream, a, grid);
+    else hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, false, true, OUT>), wgs, threads, lds, stream, a, grid);
 }
 template <Mode MODE, int RT>
-hipError_t go(const MxProductArgs& a, bool out_f32, hipStream_t stream) {
-    out_f32 ? go<MODE, RT, float>(a, stream) : go<MODE, RT, bf16_t>(a, stream);
+hipError_t go(const MxProductArgs& a, bool vec, bool out_f32, hipStream_t stream) {
+    out_f32 ? go<MODE, RT, float>(a, vec, stream) : go<MODE, RT, bf16_t>(a, vec, stream);
     return hipGetLastError();
 }
 
 bool fits(const MxProductArgs& a, uint32_t outs) {           // places within 31 bits, and a launch of less than 2^31 threads
-    return a.rows_vec && a.row_stride < (1u << 23) && (a.cap / 128 + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(outs) + kTile - 1) / kTile + 8) < (1u << 21);
+    return a.row_stride < (1u << 23) && (a.cap / 128 + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(outs) + kTile - 1) / kTile + 8) < (1u << 21);
 }
 
 }  // namespace
 
-bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) { return fits(a, a.N) && (!mx_rows || a.row_scales_stride < (1u << 22)); }
+bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) { return fits(a, a.N) && (!mx_rows || (a.rows_vec && a.row_scales_stride < (1u << 22))); }
 hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool half, bool out_f32, hipStream_t stream) {
-    if (mx_rows) return go<kMxRows, 2>(a, out_f32, stream);
-    return half ? go<kBf16Rows, 1>(a, out_f32, stream) : go<kBf16Rows, 2>(a, out_f32, stream);
+    if (mx_rows) return go<kMxRows, 2>(a, true, out_f32, stream);
+    // (256 rows that come through registers are more than there are)
+    return half || !a.rows_vec ? go<kBf16Rows, 1>(a, a.rows_vec, out_f32, stream) : go<kBf16Rows, 2>(a, true, out_f32, stream);
 }
 
-// (d_out's rows are whole 16-byte pieces: of one that reaches past a row's end the rest would be multiplied)
-bool mx_wide_grad_takes(const MxProductArgs& a) { return fits(a, a.K) && a.N % 8 == 0; }
+bool mx_wide_grad_takes(const MxProductArgs& a) { return fits(a, a.K) && a.N >= 8; }
 hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool half, bool out_f32, hipStream_t stream) {
-    return half ? go<kGradRows, 1>(a, out_f32, stream) : go<kGradRows, 2>(a, out_f32, stream);
+    const bool vec = a.rows_vec && a.N % 8 == 0;
+    return half ? go<kGradRows, 1>(a, vec, out_f32, stream) : go<kGradRows, 2>(a, vec, out_f32, stream);
 }
 
 }  // namespace fluxmoe
