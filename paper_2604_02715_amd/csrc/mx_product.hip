@@ -461,8 +461,8 @@ void pick_stream(const MxProductArgs& a, hipStream_t stream) {
 // their weights are read once (8 experts of 16 rows, 4096 columns, 28672 outputs: 156 -> 133 us, rows in 4 bits 134 -> 111; 12.8 rows level).
 constexpr uint32_t kTwoTiles = 9;
 
-// Workgroups of the wide tiles of `rows` rows; a tile is expected for each expert
-uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) { return std::max<uint64_t>(a.cap / rows, std::min(a.cap, a.E)) * ((outs + 255) / 256); }
+// Workgroups of the wide tiles of `rows` rows that a call is expected to have: an expert's last tile is half full
+uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) { return (a.cap / rows + std::min(a.cap, a.E) / 2) * ((uint64_t(outs) + 255) / 256); }
 
 // The wide tiles take over where the matrix cores bound the call, by the rows to an expert on average. Times in us, streamed / wide tiles of 128 rows /
 // of 256, 160 experts of 1536 columns and 5120 outputs (and turned round for the gradient):
@@ -470,20 +470,22 @@ uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
 //   4 bits         151 /  - / 207   159 /  - / 216   180 /  - / 224   279 /  - / 254  433 /  - / 311      (80: 246 / 234)
 //   BF16           171 / 215 / 278  235 / 252 / 288  292 / 269 / 308    - / 409 / 408   - / 631 / 558
 //   gradient       243 / 273 / 346  394 / 288 / 355  537 / 356 / 386    - / 504 / 447   - / 788 / 568
-// and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns (128 workgroups) 152 / 186 / 207 with BF16 rows, 200 rows
-// - / 196 / 315.
+// and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns 152 / 186 / 207 with BF16 rows; of 256 columns, 1024
+// outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 / - / 31.  Tiles of 128 rows also where those of
+// 256 would be two rounds or three with the last one far from full (BF16; same layer: 512 rows 522 / 625, 700 rows 580 / 654, 1000 rows 845 / 910; 28672 outputs,
+// 300 rows 587 / 541), for the gradient where they are one round (28672 outputs of 4096 columns: 150 rows 430 / 540, 300 rows 868 / 612).
 template <typename OUT>
 hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
     if (mx_rows) {
-        if (per_expert > 64 && mx_wide_takes(a, true)) return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
+        if (per_expert > 64 && wide_workgroups(a, 256, a.N) >= 96 && mx_wide_takes(a, true)) return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
         if (!a.rows_vec) go_stream<2, 4, 4, true, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, true, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, true, OUT>(a, stream);
         else pick_stream<1, true, OUT>(a, stream);
     } else {
-        if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 192 && mx_wide_takes(a, false))
-            return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 256, sizeof(OUT) == 4, stream);
+        if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 176 && mx_wide_takes(a, false))
+            return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 640, sizeof(OUT) == 4, stream);
         if (!a.rows_vec) go_stream<2, 4, 4, false, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, false, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, false, OUT>(a, stream);
@@ -495,9 +497,11 @@ hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
 template <typename OUT>
 hipError_t product_grad(const MxProductArgs& a, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
-    if (per_expert > 32 && wide_workgroups(a, 128, a.K) >= 64 && mx_wide_grad_takes(a))
-        return launch_mx_wide_grad(a, per_expert <= 80, sizeof(OUT) == 4, stream);
     const bool vec = a.rows_vec && a.N % 8 == 0;
+    // Rows through registers make longer steps: 160 experts of 5119 outputs, 40 rows each, streamed 422, wide 820; 90 rows 752; 110 rows 1177 in
+    // tiles of 128, 1464 of 256.
+    if (per_expert > (vec ? 32 : 128) && wide_workgroups(a, 128, a.K) >= 96 && mx_wide_grad_takes(a))
+        return launch_mx_wide_grad(a, per_expert <= (vec ? 80 : 256) || wide_workgroups(a, 128, a.K) <= 256, sizeof(OUT) == 4, stream);
     if (per_expert >= kTwoTiles) vec ? go_stream_grad<2, true, OUT>(a, stream) : go_stream_grad<2, false, OUT>(a, stream);
     else vec ? go_stream_grad<1, true, OUT>(a, stream) : go_stream_grad<1, false, OUT>(a, stream);
     return hipGetLastError();
