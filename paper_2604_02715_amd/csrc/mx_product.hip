@@ -32,16 +32,15 @@ __device__ __forceinline__ void store_outputs(const MxProductArgs& a, uint32_t r
 }
 
 // ---------------------------------------------------------------- few rows to an expert: bound by the weights' bytes
-// A wavefront has 16 MI rows and 16 NI outputs; a workgroup four of them, side by side (KS 1) or with a quarter of the columns each
-// (KS 4), 512 at a time.  Lane (r, q) of a wavefront holds blocks q, 4 + q, 8 + q and 12 + q of output r's 512 columns, as they lie in
-// memory: 16 bytes of codes and a scale each.  Which columns a matrix instruction's k numbers stand for is free as long as both
-// operands agree, so the weights go from memory to registers to the matrix cores with nothing between; a row's columns are
-// loaded likewise.  A load takes 64 bytes of each of 16 outputs, and the next one the other half of their lines, which it finds in the first
-// cache: 647 MB of 160 experts 132 us, 198 where loads pass it by, 141 where a lane's four blocks lie next to each other.
-// WHOLE: a row's scales are read as words.
-template <int MI, int NI, int KS, bool MX, bool VEC, bool WHOLE, typename OUT>
+// A workgroup has 16 MI rows and 16 NI outputs, and its four wavefronts a quarter of the columns each, 512 at a time.  Lane (r, q) of a
+// wavefront holds blocks q, 4 + q, 8 + q and 12 + q of output r's 512 columns, as they lie in memory: 16 bytes of codes and a scale
+// each.  Which columns a matrix instruction's k numbers stand for is free as long as both operands agree, so the weights go from memory
+// to registers to the matrix cores with nothing between; a row's columns are loaded likewise.  A load takes 64 bytes of each of 16
+// outputs, and the next one the other half of their lines, which it finds in the first cache: 647 MB of 160 experts 132 us, 198 where
+// loads pass it by, 141 where a lane's four blocks lie next to each other.
+// VEC: rows at 16-byte addresses, not too far apart.  WHOLE: a row's scales are read as words.
+template <int MI, int NI, bool MX, bool VEC, bool WHOLE, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
-    constexpr uint32_t kWidth = 16 * NI * 4 / KS;            // outputs of a workgroup
     __shared__ uint32_t s_tile[kTileWords];
     __shared__ f32x4 s_acc[4][MI * NI][64];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
@@ -50,8 +49,8 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
         const auto [tile_at, strip] = item_at(item, strips);
         const Tile t = find_tile<kThreads>(a, 16 * MI, tile_at, s_tile);
         if (t.rows == 0) return;                         // nor are there any behind it
-        const uint32_t n0 = strip * kWidth + (KS == 1 ? wave * (16 * NI) : 0), outs = n0 < a.N ? min(a.N - n0, uint32_t(16 * NI)) : 0;
-        const uint64_t w_row = uint64_t(t.expert) * a.N + min(n0, a.N - 1);
+        const uint32_t n0 = strip * (16 * NI), outs = min(a.N - n0, uint32_t(16 * NI));
+        const uint64_t w_row = uint64_t(t.expert) * a.N + n0;
         const row_t w = bytes_at(a.w, w_row * (a.K / 2), outs * (a.K / 2));
         const row_t ws = bytes_at(a.ws, w_row * blocks, outs * blocks);
 
@@ -61,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
 #pragma unroll
             for (int n = 0; n < NI; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
 
-        for (uint32_t super = KS == 1 ? 0 : wave; super < supers; super += KS) {
+        for (uint32_t super = wave; super < supers; super += 4) {
             const uint32_t block = super * 16 + q;           // and 4, 8, 12 behind it
             u32x4 wv[NI][4];
             uint32_t wsv[NI];
@@ -86,9 +85,16 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
 #pragma unroll
                 for (int m = 0; m < MI; ++m) {
                     xs[m] = 0;
-                    if (have[m])
-                        xs[m] = spread_scales<WHOLE>(bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks),
-                                                     (m * 16 + r) * uint32_t(a.row_scales_stride), block, q, blocks);
+                    if constexpr (WHOLE) {
+                        if (have[m])
+                            xs[m] = spread_scales<true>(bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks),
+                                                        (m * 16 + r) * uint32_t(a.row_scales_stride), block, q, blocks);
+                    } else {
+                        const uint8_t* scales = a.row_scales + uint64_t(t.first + (have[m] ? m * 16 + r : 0)) * a.row_scales_stride;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (have[m] && block + 4 * i < blocks) xs[m] |= uint32_t(scales[block + 4 * i]) << (8 * i);
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         xv[m][i] = u32x4{0, 0, 0, 0};
@@ -143,22 +149,19 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
             }
         }
 
-        // The quarters' sums in their order (KS 4); then neighbouring threads have neighbouring outputs of a row, four to each.
+        // The quarters' sums in their order; then neighbouring threads have neighbouring outputs of a row, four to each.
 #pragma unroll
         for (int m = 0; m < MI; ++m)
 #pragma unroll
             for (int n = 0; n < NI; ++n) s_acc[wave][m * NI + n][lane] = acc[m][n];
-        if constexpr (KS == 1) wave_fence();
-        else __syncthreads();
-        for (uint32_t i = KS == 1 ? lane : tid; i < 64 * MI * NI; i += KS == 1 ? 64 : kThreads) {
+        __syncthreads();
+        for (uint32_t i = tid; i < 64 * MI * NI; i += kThreads) {
             const uint32_t row = i / (4 * NI), quad = i % (4 * NI);
             if (row >= t.rows) break;
             const uint32_t at = (quad & 3) * 16 + (row & 15), part = (row >> 4) * NI + (quad >> 2);
-            f32x4 v = s_acc[KS == 1 ? wave : 0][part][at];
-            if constexpr (KS > 1) {
+            f32x4 v = s_acc[0][part][at];
 #pragma unroll
-                for (int k = 1; k < KS; ++k) v += s_acc[k][part][at];
-            }
+            for (int k = 1; k < 4; ++k) v += s_acc[k][part][at];
             if (quad * 4 < outs) store_outputs<OUT>(a, t.first + row, n0 + quad * 4, min(outs - quad * 4, 4u), v);
         }
     }
@@ -417,13 +420,15 @@ bool whole_scales(const MxProductArgs& a) {
     const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
     return words(a.ws, a.K / kMxBlock) && (!MX || words(a.row_scales, a.row_scales_stride));
 }
-template <int MI, int NI, int KS, bool MX, bool VEC, typename OUT>
+// 64 rows' places, counted from the first one's, within 31 bits
+bool near_rows(const MxProductArgs& a, bool mx_rows) { return a.row_stride < (1u << 24) && (!mx_rows || a.row_scales_stride < (1u << 24)); }
+template <int MI, int NI, bool MX, bool VEC, typename OUT>
 void go_stream(const MxProductArgs& a, hipStream_t stream) {
-    const Plan p(a, 16 * MI, a.N, 16 * NI * 4 / KS);
+    const Plan p(a, 16 * MI, a.N, 16 * NI);
     if (VEC && whole_scales<MX>(a))
-        hipLaunchKernelGGL((mx_stream_kernel<MI, NI, KS, MX, VEC, VEC, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+        hipLaunchKernelGGL((mx_stream_kernel<MI, NI, MX, VEC, VEC, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
     else
-        hipLaunchKernelGGL((mx_stream_kernel<MI, NI, KS, MX, VEC, false, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+        hipLaunchKernelGGL((mx_stream_kernel<MI, NI, MX, VEC, false, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
 }
 template <int MI, bool VEC, typename OUT>
 void go_stream_grad(const MxProductArgs& a, hipStream_t stream) {
@@ -454,8 +459,8 @@ void pick_stream(const MxProductArgs& a, hipStream_t stream) {
     constexpr int kStrip = MX || MI == 2 ? 4 : 2;            // sixteens of outputs to a wavefront
     if constexpr (MI == 4) go_strip<MI, kStrip, MX, OUT>(a, whole_scales<MX>(a), stream);
     else if ((!MX || a.K <= 2048) && tiles * (a.N / (64 * kStrip)) >= 448) go_strip<MI, kStrip, MX, OUT>(a, whole_scales<MX>(a), stream);
-    else if (tiles * (a.N / 64) >= 512) go_stream<MI, 4, 4, MX, true, OUT>(a, stream);
-    else go_stream<MI, 1, 4, MX, true, OUT>(a, stream);
+    else if (tiles * (a.N / 64) >= 512) go_stream<MI, 4, MX, true, OUT>(a, stream);
+    else go_stream<MI, 1, MX, true, OUT>(a, stream);
 }
 // Two 16-row tiles of rows to a workgroup from this many rows for each expert on, on average: some experts have more than 16 then, and
 // their weights are read once (8 experts of 16 rows, 4096 columns, 28672 outputs: 156 -> 133 us, rows in 4 bits 134 -> 111; 12.8 rows level).
@@ -479,14 +484,14 @@ hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
     if (mx_rows) {
         if (per_expert > 64 && wide_workgroups(a, 256, a.N) >= 96 && mx_wide_takes(a, true)) return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
-        if (!a.rows_vec) go_stream<2, 4, 4, true, false, OUT>(a, stream);
+        if (!a.rows_vec || !near_rows(a, true)) go_stream<2, 4, true, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, true, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, true, OUT>(a, stream);
         else pick_stream<1, true, OUT>(a, stream);
     } else {
         if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 176 && mx_wide_takes(a, false))
             return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 640, sizeof(OUT) == 4, stream);
-        if (!a.rows_vec) go_stream<2, 4, 4, false, false, OUT>(a, stream);
+        if (!a.rows_vec || !near_rows(a, false)) go_stream<2, 4, false, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, false, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, false, OUT>(a, stream);
         else pick_stream<1, false, OUT>(a, stream);

@@ -275,6 +275,44 @@ def test_places_past_32_bits(count, mx):
         assert bool((out[:-count] == 7.0).all())
 
 
+@pytest.mark.parametrize("mx", [False, True])
+def test_rows_far_apart(mx):
+    """rows more than 4 GB apart, places that no 32 bits hold within a tile"""
+    n, N, K, stride = 3, 40, 64, (1 << 32) + 16 if mx else (1 << 31) + 8
+    offsets, counts, _ = plain.groups([1, 2])
+    wc, ws = plain.random_weights(2, N, K, 1)
+    x, xs, x64 = rows_in(n, K, mx, 2)
+    far = torch.empty((n - 1) * stride + K, dtype=x.dtype, device="cuda").as_strided((n, x.shape[1]), (stride, 1))
+    far.copy_(x)
+    if mx:
+        scales = torch.empty((n - 1) * ((1 << 31) + 4) + 4, dtype=torch.uint8, device="cuda").as_strided((n, K // 32), ((1 << 31) + 4, 1))
+        scales.copy_(xs)
+        xs = scales
+    out = torch.full((n, N), 7.0, device="cuda")
+    X.product(far, offsets, counts, wc, ws, out, row_scales=xs)
+    near(out, *plain.products(x64, offsets, counts, plain.values(wc, ws)), K)
+    if not mx:
+        d, _, d64 = rows_in(n, N, False, 3)
+        whole = torch.full(((n - 1) * stride + K,), 7.0, dtype=BF16, device="cuda")
+        back = whole.as_strided((n, K), (stride, 1))
+        X.product_grad(d, offsets, counts, wc, ws, back)
+        near(back, *plain.products(d64, offsets, counts, plain.values(wc, ws), transposed=True), N)
+        far = whole.as_strided((n, N), (stride, 1))
+        far.copy_(d)
+        back = torch.full((n, K), 7.0, device="cuda")
+        X.product_grad(far, offsets, counts, wc, ws, back)
+        near(back, *plain.products(d64, offsets, counts, plain.values(wc, ws), transposed=True), N)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_most_experts(mx):
+    counts = [0] * 4096
+    for e, c in ((0, 1), (15, 2), (16, 17), (1000, 1), (1001, 3), (4095, 5)):
+        counts[e] = c
+    check(counts, 24, 64, mx, F32)
+    check_grad(counts, 24, 64, F32)
+
+
 def test_other_stream():
     offsets, counts, n = plain.groups([5, 60])
     wc, ws = plain.random_weights(2, 64, 128, 1)
