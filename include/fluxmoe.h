@@ -589,7 +589,7 @@ int fluxmoe_mx_dequantize(const uint8_t* codes, uint64_t codes_stride, const uin
  *   rows     rows_type FLUXMOE_BF16 [rows_cap][K], or FLUXMOE_MXFP4: codes with row_scales [rows_cap][K / 32]
  *   out      out_type FLUXMOE_BF16 or FLUXMOE_F32 [rows_cap][N], not overlapping the rows; sums are FP32 and rounded once
  * Strides are in elements (codes and scales: bytes) from one row to the next; 0: the row's width.  Rows at other than
- * 16-byte addresses, or with N not a multiple of 8 for the gradient, take kernels that are slower, up to three times.
+ * 16-byte addresses, for the gradient also with N not a multiple of 8, take slower kernels.
  */
 typedef struct {
     uint32_t E, N, K;
@@ -606,8 +606,9 @@ int fluxmoe_mx_product_grad(const fluxmoe_mx_product_desc* desc, const uint16_t*
                             const int32_t* counts, const uint8_t* w_codes, const uint8_t* w_scales, void* d_rows, void* stream);
 
 /* Between an expert's products: h[r][f] = g / (1 + e^-g) * u with g = gate_up[r][f], u = gate_up[r][ffn + f] (`type`
- * [rows][2 ffn], h h_type [rows][ffn], not overlapping; strides in elements).  And its gradient: d_gate_up, of gate_up's type, from d_h, of
- * h's; it may be gate_up's own rows (then with their stride).  Rows that belong to no expert are passed through like the others. */
+ * [rows][2 ffn], h h_type [rows][ffn] elsewhere; strides in elements).  And its gradient: d_gate_up, of gate_up's type,
+ * from d_h, of h's; it may be gate_up's own rows (then with their stride), otherwise all three lie apart.  Rows that
+ * belong to no expert are passed through like the others. */
 int fluxmoe_swiglu(const void* gate_up, uint32_t type, uint64_t rows, uint32_t ffn, uint64_t gate_up_stride, void* h,
                    uint32_t h_type, uint64_t h_stride, void* stream);
 int fluxmoe_swiglu_grad(const void* gate_up, uint32_t type, uint64_t rows, uint32_t ffn, uint64_t gate_up_stride,

@@ -100,6 +100,10 @@ __device__ __forceinline__ row_t bytes_at(const void* base, uint64_t offset, uin
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + offset), 0, int(records), 0x00020000);
 }
 constexpr uint32_t kNowhere = 0x7FFFFFF0u;               // an offset past any resource's records
+// 16 bytes, or 0 where there are none
+__device__ __forceinline__ u32x4 piece_at(row_t m, bool there, uint32_t offset) {
+    return __builtin_amdgcn_raw_buffer_load_b128(m, there ? offset : kNowhere, 0, kCached);
+}
 
 __device__ __forceinline__ float scale_operand(uint32_t s) { return __uint_as_float(s << 23); }
 

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
                 const uint32_t row = n * 16 + r;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    wv[n][i] = __builtin_amdgcn_raw_buffer_load_b128(w, block + 4 * i < blocks ? row * (a.K / 2) + (block + 4 * i) * 16 : kNowhere, 0, kCached);
+                    wv[n][i] = piece_at(w, block + 4 * i < blocks, row * (a.K / 2) + (block + 4 * i) * 16);
                 wsv[n] = spread_scales<WHOLE>(ws, row * blocks, block, q, blocks);
             }
             const char* src[MI];
@@ -86,9 +86,9 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
                 for (int m = 0; m < MI; ++m) {
                     xs[m] = 0;
                     if constexpr (WHOLE) {
-                        if (have[m])
-                            xs[m] = spread_scales<true>(bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks),
-                                                        (m * 16 + r) * uint32_t(a.row_scales_stride), block, q, blocks);
+                        const uint32_t stride = uint32_t(a.row_scales_stride);
+                        const row_t scales = bytes_at(a.row_scales, uint64_t(t.first) * stride, (t.rows - 1) * stride + blocks);
+                        if (have[m]) xs[m] = spread_scales<true>(scales, (m * 16 + r) * stride, block, q, blocks);
                     } else {
                         const uint8_t* scales = a.row_scales + uint64_t(t.first + (have[m] ? m * 16 + r : 0)) * a.row_scales_stride;
 #pragma unroll
@@ -167,10 +167,10 @@ __global__ __launch_bounds__(kThreads) void mx_stream_kernel(MxProductArgs a, ui
     }
 }
 
-// The same for more bytes: four wavefronts side by side, 64 outputs each, over all columns.  The rows' columns come through LDS, for all four, and
-// the weights of the next 256 columns are on their way while these are multiplied: loads return in the order of their issue, so rows that a
-// wavefront fetched for itself would be waited for behind those weights.  A row's 16-byte pieces are placed so that 16 rows' pieces of one
-// number lie in different banks.
+// The same for more bytes: four wavefronts side by side, 16 NI outputs each, over all columns.  The rows' columns come through LDS, for all
+// four, and the weights of the next 256 columns are on their way while these are multiplied: loads return in the order of their issue, so
+// rows that a wavefront fetched for itself would be waited for behind those weights.  A row's 16-byte pieces are placed so that 16 rows'
+// pieces of one number lie in different banks.
 template <int MI, int NI, bool MX, bool WHOLE, typename OUT>
 __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
     constexpr uint32_t kPieces = MX ? 8 : 32;                // 16-byte pieces of a row's 256 columns
@@ -188,7 +188,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
         const uint64_t w_row = uint64_t(t.expert) * a.N + min(n0, a.N - 1);
         const row_t w = bytes_at(a.w, w_row * (a.K / 2), outs * (a.K / 2)), ws = bytes_at(a.ws, w_row * blocks, outs * blocks);
         const row_t x = bytes_at(a.rows, uint64_t(t.first) * a.row_stride, (t.rows - 1) * uint32_t(a.row_stride) + (MX ? a.K / 2 : a.K * 2));
-        const row_t xs = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
+        const row_t xs = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride,
+                                  MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
 
         auto swizzle = [](uint32_t row) __attribute__((always_inline)) { return MX ? (row >> 1) & 7 : row & 15; };
         struct Operands {
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
 #pragma unroll
             for (int c = 0; c < kMine; ++c) {                // ahead of the weights, to be waited for without them
                 const uint32_t at = tid + c * kThreads, row = at / kPieces, piece = step * kPieces + at % kPieces;
-                mine[c] = __builtin_amdgcn_raw_buffer_load_b128(x, row < t.rows && piece < blocks * (MX ? 1 : 4) ? row * uint32_t(a.row_stride) + piece * 16 : kNowhere, 0, kCached);
+                mine[c] = piece_at(x, row < t.rows && piece < blocks * (MX ? 1 : 4), row * uint32_t(a.row_stride) + piece * 16);
             }
             const uint32_t block = step * 8 + q;
             if constexpr (MX) {
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
                 o.ws[n] = pair_scales<WHOLE>(ws, row * blocks, block, q, blocks);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    o.w[n][i] = __builtin_amdgcn_raw_buffer_load_b128(w, block + 4 * i < blocks ? row * (a.K / 2) + (block + 4 * i) * 16 : kNowhere, 0, kCached);
+                    o.w[n][i] = piece_at(w, block + 4 * i < blocks, row * (a.K / 2) + (block + 4 * i) * 16);
             }
         };
         auto put = [&](uint32_t stage) __attribute__((always_inline)) {
@@ -254,7 +255,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
                     for (int j = 0; j < 4; ++j) {
                         bf16x8 xv[MI];
 #pragma unroll
-                        for (int m = 0; m < MI; ++m) xv[m] = __builtin_bit_cast(bf16x8, s_x[stage][(m * 16 + r) * kPieces + ((16 * i + 4 * q + j) ^ swizzle(r))]);
+                        for (int m = 0; m < MI; ++m)
+                            xv[m] = __builtin_bit_cast(bf16x8, s_x[stage][(m * 16 + r) * kPieces + ((16 * i + 4 * q + j) ^ swizzle(r))]);
 #pragma unroll
                         for (int n = 0; n < NI; ++n) {
                             const bf16x8 f = codes_bf16(o.w[n][i][j], scale[n]);
@@ -302,9 +304,9 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
     }
 }
 
-// The gradient likewise.  A workgroup has 16 MI rows and 256 columns, its four or eight wavefronts share out the outputs, 32 at a time.  Lane (r, q)
-// loads 16 neighbouring columns of eight outputs, eight bytes of each, turns them into sixteen fragments of eight outputs by a conversion and
-// a permutation to each two numbers, and fragment c goes to a matrix instruction whose results are column c of every lane's.
+// The gradient likewise.  A workgroup has 16 MI rows and 256 columns, its four or eight wavefronts share out the outputs, 32 at a time.
+// Lane (r, q) loads 16 neighbouring columns of eight outputs, eight bytes of each, turns them into sixteen fragments of eight outputs by a
+// conversion and a permutation to each two numbers, and fragment c goes to a matrix instruction whose results are column c of every lane's.
 template <int MI, int WAVES, bool VEC, typename OUT>
 __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
     __shared__ uint32_t s_tile[kTileWords];
@@ -337,7 +339,8 @@ __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArg
 #pragma unroll
             for (int m = 0; m < MI; ++m) {
                 x[m] = u32x4{0, 0, 0, 0};
-                const uint16_t* p = reinterpret_cast<const uint16_t*>(static_cast<const char*>(a.rows) + uint64_t(t.first + min(m * 16 + r, t.rows - 1)) * a.row_stride) + n;
+                const uint64_t at = uint64_t(t.first + min(m * 16 + r, t.rows - 1)) * a.row_stride;
+                const uint16_t* p = reinterpret_cast<const uint16_t*>(static_cast<const char*>(a.rows) + at) + n;
                 if (m * 16 + r < t.rows) {
                     if (VEC && n < a.N) x[m] = *reinterpret_cast<const u32x4*>(p);
                     if constexpr (!VEC) {
@@ -433,8 +436,9 @@ void go_stream(const MxProductArgs& a, hipStream_t stream) {
 template <int MI, bool VEC, typename OUT>
 void go_stream_grad(const MxProductArgs& a, hipStream_t stream) {
     const Plan p(a, 16 * MI, a.K, 256);
-    // Eight wavefronts where there are fewer than four workgroups for a CU: 160 experts, 13 rows each, 1536 columns 185 -> 162 us, 8 experts, 16 rows,
-    // 4096 columns of 28672 outputs 369 -> 217; with more workgroups the longer sum at the end costs more (512 experts, 512 columns 90 -> 95).
+    // Eight wavefronts where there are fewer than four workgroups for a CU: 160 experts, 13 rows each, 1536 columns 185 -> 162 us,
+    // 8 experts, 16 rows, 4096 columns of 28672 outputs 369 -> 217; with more workgroups the longer sum at the end costs more
+    // (512 experts, 512 columns 90 -> 95).
     if (std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E)) * p.strips < 4 * 256)
         hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 8, VEC, OUT>), dim3(p.grid), dim3(512), 0, stream, a, p.strips, p.items);
     else
@@ -448,8 +452,9 @@ void go_strip(const MxProductArgs& a, bool whole, hipStream_t stream) {
 }
 
 // Which of the three. Times in us, 16-bit outputs, even routing but for 512 experts:
-//   rows in 4 bits, side by side / quarters: 512 columns (512 experts, 900 tokens) 88 / 203, 1536 (160, 256) 143 / 167, 2048 (512, 256) 100 / 106,
-//   4096 (8, 64) 154 / 134, 5120 (160, 16) 151 / 116: long rows are better read a whole piece at a time, and there are more workgroups;
+//   rows in 4 bits, side by side / quarters: 512 columns (512 experts, 900 tokens) 88 / 203, 1536 (160, 256) 143 / 167,
+//   2048 (512, 256) 100 / 106, 4096 (8, 64) 154 / 134, 5120 (160, 16) 151 / 116: long rows are better read a whole piece at a time, and
+//   there are more workgroups;
 //   BF16 rows, which quarters fetch for every 64 outputs: 1536 (160, 256) 153 / 253, 5120 (160, 16) 145 / 156;
 //   BF16 rows, 32 / 64 outputs to a wavefront: one tile of rows 153 / 159 (1536), 145 / 155 (5120), two 176 / 171.
 // Where the workgroups would be few, narrow ones with a quarter each (one token of 512 experts, 2048 columns, 1024 outputs 7.7).
@@ -467,23 +472,27 @@ void pick_stream(const MxProductArgs& a, hipStream_t stream) {
 constexpr uint32_t kTwoTiles = 9;
 
 // Workgroups of the wide tiles of `rows` rows that a call is expected to have: an expert's last tile is half full
-uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) { return (a.cap / rows + std::min(a.cap, a.E) / 2) * ((uint64_t(outs) + 255) / 256); }
+uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
+    return (a.cap / rows + std::min(a.cap, a.E) / 2) * ((uint64_t(outs) + 255) / 256);
+}
 
-// The wide tiles take over where the matrix cores bound the call, by the rows to an expert on average. Times in us, streamed / wide tiles of 128 rows /
-// of 256, 160 experts of 1536 columns and 5120 outputs (and turned round for the gradient):
+// The wide tiles take over where the matrix cores bound the call, by the rows to an expert on average. Times in us, streamed / wide tiles
+// of 128 rows / of 256, 160 experts of 1536 columns and 5120 outputs (and turned round for the gradient):
 //   rows           26               40               60               120             200
 //   4 bits         151 /  - / 207   159 /  - / 216   180 /  - / 224   279 /  - / 254  433 /  - / 311      (80: 246 / 234)
 //   BF16           171 / 215 / 278  235 / 252 / 288  292 / 269 / 308    - / 409 / 408   - / 631 / 558
 //   gradient       243 / 273 / 346  394 / 288 / 355  537 / 356 / 386    - / 504 / 447   - / 788 / 568
-// and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns 152 / 186 / 207 with BF16 rows; of 256 columns, 1024
-// outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 / - / 31.  Tiles of 128 rows also where those of
-// 256 would be two rounds or three with the last one far from full (BF16; same layer: 512 rows 522 / 625, 700 rows 580 / 654, 1000 rows 845 / 910; 28672 outputs,
-// 300 rows 587 / 541), for the gradient where they are one round (28672 outputs of 4096 columns: 150 rows 430 / 540, 300 rows 868 / 612).
+// and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns 152 / 186 / 207 with BF16 rows; of 256
+// columns, 1024 outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 /  - / 31.  Tiles of 128 rows also where those of
+// 256 would be two rounds or three with the last one far from full (BF16, 128 / 256; same layer: 512 rows 522 / 625, 700 rows 580 / 654,
+// 1000 rows 845 / 910; 28672 outputs, 300 rows 587 / 541), for the gradient where they are one round (28672 outputs of 4096 columns:
+// 150 rows 430 / 540, 300 rows 868 / 612).
 template <typename OUT>
 hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
     if (mx_rows) {
-        if (per_expert > 64 && wide_workgroups(a, 256, a.N) >= 96 && mx_wide_takes(a, true)) return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
+        if (per_expert > 64 && wide_workgroups(a, 256, a.N) >= 96 && mx_wide_takes(a, true))
+            return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
         if (!a.rows_vec || !near_rows(a, true)) go_stream<2, 4, true, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, true, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, true, OUT>(a, stream);

@@ -40,9 +40,10 @@ struct WideGrid {
     }
 };
 
-// 16 (4) bytes to each lane's place of the KiB (256 bytes) at lds_addr, from its offset to the wavefront's base.  Assembly on purpose: with the compiler's builtin every later LDS read
-// waits for all loads into LDS that are under way, as it cannot tell that they fill another stage.  The waits are those written below, ahead of
-// the barriers.  M0 holds the destination; the compiler has reserved it, so its value is put back.
+// 16 (4) bytes to each lane's place of the KiB (256 bytes) at lds_addr, from its offset to the wavefront's base.  Assembly on purpose: with
+// the compiler's builtin every later LDS read waits for all loads into LDS that are under way, as it cannot tell that they fill another
+// stage.  The waits are those written below, ahead of the barriers.  M0 holds the destination; the compiler has reserved it, so its value
+// is put back.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds_addr) {
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
@@ -63,8 +64,9 @@ enum Mode { kMxRows, kBf16Rows, kGradRows };
 constexpr int kRawScales = kTile * 8;                    // bytes of a superblock's scales
 constexpr int scale_bytes(Mode mode) { return mode == kMxRows ? 4 * kRawScales : 2 * kRawScales + (mode == kGradRows ? 2 * kScaleStage : 0); }
 
-// RT: 32-row groups of a wavefront, 2 for tiles of 256 rows and 1 for 128, whose columns are fetched four steps ahead in as much LDS as two take there.
-// WHOLE: scales are read four at a time.  VEC: the rows are whole 16-byte pieces at 16-byte addresses; others come through registers.
+// RT: 32-row groups of a wavefront, 2 for tiles of 256 rows and 1 for 128, whose columns are fetched four steps ahead in as much LDS as two
+// take there.  WHOLE: scales are read four at a time.  VEC: the rows are whole 16-byte pieces at 16-byte addresses; others come through
+// registers.
 template <Mode MODE, int RT, bool WHOLE, bool VEC, typename OUT>
 __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, WideGrid grid) {
     constexpr bool MX = MODE == kMxRows, GRAD = MODE == kGradRows;
@@ -124,7 +126,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     u32x4 held[VEC ? 1 : kXLoads];
     auto hold_x = [&](int i, uint32_t super, uint32_t s) __attribute__((always_inline)) {
         const uint32_t sum = GRAD ? a.N : a.K;
-        const uint32_t column = GRAD ? super * 256 + s * 64 + piece_of(i) * 8 : (super * 8 + s + 4 * (piece_of(i) >> 2)) * 32 + (piece_of(i) & 3) * 8;
+        const uint32_t column =
+            GRAD ? super * 256 + s * 64 + piece_of(i) * 8 : (super * 8 + s + 4 * (piece_of(i) >> 2)) * 32 + (piece_of(i) & 3) * 8;
         const uint32_t from = min(column, sum - 8), beyond = min(column - from, 8u);
         uint64_t v[2];
         __builtin_memcpy(v, x_base + x_off[i] + from * 2, 16);
@@ -139,7 +142,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     };
 
     const row_t ws_at = bytes_at(a.ws, (uint64_t(t.expert) * a.N + n0) * blocks, GRAD ? 0 : min(kTile, a.N - n0) * blocks);
-    const row_t xs_at = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride, MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
+    const row_t xs_at = bytes_at(a.row_scales, uint64_t(t.first) * a.row_scales_stride,
+                                 MX ? (t.rows - 1) * uint32_t(a.row_scales_stride) + blocks : 0);
     auto w_scales = [&](int j, uint32_t super) __attribute__((always_inline)) {
         return four_scales<WHOLE>(ws_at, min(wn * 128 + j * 32 + q, a.N - 1 - n0) * blocks, super * 8 + 4 * h, blocks);
     };
@@ -167,13 +171,11 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
     // each of 32 rows at a time, they were a third of a step: 16382 rows in 4 bits of 14336 columns, 4096 outputs 822 us, through LDS 572.)
     auto fetch_words = [&](uint32_t super) __attribute__((always_inline)) {
         const uint32_t row = tid >> 1, to = lds_base + 4 * kStage + (GRAD ? 2 * kScaleStage : 0) + (super & 1) * kRawScales + wave * 256;
+        const uint32_t first = GRAD ? super * 256 : n0, block = min((GRAD ? n0 / kMxBlock : super * 8) + 4 * (tid & 1), blocks - 4);
         if constexpr (MX)
-            load_word_to_lds(a.row_scales + uint64_t(t.first) * a.row_scales_stride, min(row, t.rows - 1) * uint32_t(a.row_scales_stride) + min(super * 8 + 4 * (tid & 1), blocks - 4),
+            load_word_to_lds(a.row_scales + uint64_t(t.first) * a.row_scales_stride, min(row, t.rows - 1) * uint32_t(a.row_scales_stride) + block,
                              to + 2 * kRawScales);
-        if constexpr (GRAD)
-            load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + super * 256) * blocks, min(row, a.N - 1 - super * 256) * blocks + min(n0 / kMxBlock + 4 * (tid & 1), blocks - 4), to);
-        else
-            load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + n0) * blocks, min(row, a.N - 1 - n0) * blocks + min(super * 8 + 4 * (tid & 1), blocks - 4), to);
+        load_word_to_lds(a.ws + (uint64_t(t.expert) * a.N + first) * blocks, min(row, a.N - 1 - first) * blocks + block, to);
     };
     // the columns of a tile's first steps
     auto first_rows = [&]() __attribute__((always_inline)) {
@@ -327,9 +329,9 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             if (super + 1 < supers) step(Int<1>{}, Int<0>{}, super++);
             step(Int<0>{}, Int<0>{}, super);
         } else if constexpr (GRAD) {
-            // A superblock is 256 outputs, a step 64 of them, a sub-step eight of either half of those.  Lane q has four neighbouring columns, a 32 x 32 tile
-            // every fourth one: two bytes of codes of each of eight outputs become the tiles' fragments by a conversion and a permutation to
-            // each two numbers.  The scales lie in LDS as the conversion takes them, a block's outputs one after the other.
+            // A superblock is 256 outputs, a step 64 of them, a sub-step eight of either half of those.  Lane q has four neighbouring columns,
+            // a 32 x 32 tile every fourth one: two bytes of codes of each of eight outputs become the tiles' fragments by a conversion and a
+            // permutation to each two numbers.  The scales lie in LDS as the conversion takes them, a block's outputs one after the other.
             uint32_t scales_next = 0;
             u32x4 fx[2][RT], fw[2][4], sc[2];
             uint32_t raw[8], pair[8][2];
@@ -347,7 +349,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             };
             auto read_raw = [&](uint32_t super, int s, int ks) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) raw[j] = *reinterpret_cast<const uint16_t*>(lds + (raw_at + (super & 1) * kStage) + (64 * s + 8 * ks + j) * 128);
+                for (int j = 0; j < 8; ++j)
+                    raw[j] = *reinterpret_cast<const uint16_t*>(lds + (raw_at + (super & 1) * kStage) + (64 * s + 8 * ks + j) * 128);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) sc[j] = read(sc_at + (super & 1) * kScaleStage + (64 * s + 8 * ks + 4 * j) * 4);
             };
@@ -362,7 +365,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                     fw[set][c][d] = __builtin_amdgcn_perm(pair[2 * d + 1][c / 2], pair[2 * d][c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
             };
             auto raw_scales = [&](uint32_t super) __attribute__((always_inline)) {
-                if constexpr (WHOLE) scales_next = *reinterpret_cast<const uint32_t*>(lds + 4 * kStage + 2 * kScaleStage + (super & 1) * kRawScales + tid * 4);
+                if constexpr (WHOLE)
+                    scales_next = *reinterpret_cast<const uint32_t*>(lds + 4 * kStage + 2 * kScaleStage + (super & 1) * kRawScales + tid * 4);
                 else asm volatile("" : "+v"(scales_next));
             };
             if constexpr (WHOLE) fetch_words(0);
@@ -407,7 +411,9 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 #pragma unroll
                     for (int n = 0; n < 8; ++n) {
                         const int i = n / 4, j = n % 4;
-                        if (i < act) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), __builtin_bit_cast(bf16x8, fw[set][j]), acc[i][j], 0, 0, 0);
+                        if (i < act)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), __builtin_bit_cast(bf16x8, fw[set][j]),
+                                                                               acc[i][j], 0, 0, 0);
                         if constexpr (ahead) {
                             if (n < act) fx[set ^ 1][n] = ks < 3 ? read_x(n, ks + 1, stage) : read_x(n, 0, stage_next);
                             if (n == 2 || n == 3)
@@ -417,7 +423,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
                         }
                         // the next superblock's weights, in the first two steps of this one
                         if (ks == 0 && s < 2 && (n == 3 || n == 7) && load_w) fetch_w(s * 2 + n / 4, super + 1);
-                        if (VEC && ks == 3 && load && (n & 1) && n / 2 < kXLoads) fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
+                        if (VEC && ks == 3 && load && (n & 1) && n / 2 < kXLoads)
+                            fetch_x(n / 2, super + (s + kXStages) / 4, (s + kXStages) % 4, stage);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 };
@@ -450,8 +457,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             step(Int<2>{}, Int<0>{}, super);
             step(Int<3>{}, Int<0>{}, super);
         } else {
-            // A step is 64 columns: blocks s and 4 + s of a superblock, whose codes are in LDS for its four steps.  A sub-step is eight columns of
-            // both blocks; its weights are converted in the sub-step before.
+            // A step is 64 columns: blocks s and 4 + s of a superblock, whose codes are in LDS for its four steps.  A sub-step is eight columns
+            // of both blocks; its weights are converted in the sub-step before.
             uint32_t scales[4], scales_next[4];
             float sc[4];
             u32x4 codes[4], fx[2][RT];
@@ -466,8 +473,10 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
             };
             auto take_scales = [&](uint32_t super) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    scales[j] = WHOLE ? *reinterpret_cast<const uint32_t*>(lds + 4 * kStage + (super & 1) * kRawScales + (wn * 128 + j * 32 + q) * 8 + 4 * h) : scales_next[j];
+                for (int j = 0; j < 4; ++j) {
+                    const uint8_t* from = lds + 4 * kStage + (super & 1) * kRawScales + (wn * 128 + j * 32 + q) * 8 + 4 * h;
+                    scales[j] = WHOLE ? *reinterpret_cast<const uint32_t*>(from) : scales_next[j];
+                }
             };
             if constexpr (WHOLE) fetch_words(0);
             else fetch_scales(0);
@@ -519,7 +528,8 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 #pragma unroll
                     for (int n = 0; n < 8; ++n) {
                         const int i = n / 4, j = n % 4;
-                        if (i < act) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), fw[set][j], acc[i][j], 0, 0, 0);
+                        if (i < act)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fx[set][i]), fw[set][j], acc[i][j], 0, 0, 0);
                         if constexpr (ks < 3) {
                             if (n < act) fx[set ^ 1][n] = read_x(n, ks + 1, stage);
                             if (act > 0 && (n & 1)) fw[set ^ 1][n / 2] = codes_bf16(codes[n / 2][ks + 1], sc[n / 2]);
@@ -661,7 +671,9 @@ bool fits(const MxProductArgs& a, uint32_t outs) {           // places within 31
 
 }  // namespace
 
-bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) { return fits(a, a.N) && (!mx_rows || (a.rows_vec && a.row_scales_stride < (1u << 22))); }
+bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) {
+    return fits(a, a.N) && (!mx_rows || (a.rows_vec && a.row_scales_stride < (1u << 22)));
+}
 hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool half, bool out_f32, hipStream_t stream) {
     if (mx_rows) return go<kMxRows, 2>(a, true, out_f32, stream);
     // (256 rows that come through registers are more than there are)
