@@ -1,10 +1,11 @@
 // The product with experts' weights in 4-bit floating point where an expert has many rows: bound by the matrix cores.
 //
 // A workgroup's tile is 256 rows by 256 outputs, eight wavefronts as 4 (rows) x 2 (outputs), two to a SIMD, 64 x 128 each as
-// 2 x 4 tiles of the 32x32 matrix instructions.  Both operands go from memory straight to LDS, as they are: rows of 128 bytes, which are
-// 256 columns of codes (a superblock: eight blocks of 32, a 16-byte piece each) or 64 columns of BF16.  A load fills 1 KiB of LDS
-// without gaps, so instead of padding, the lane that fills position p of a row fetches piece p ^ ((row >> 1) & 7): 16 neighbouring
-// rows' pieces of one number then lie in 64 different banks.
+// 2 x 4 tiles of the 32x32 matrix instructions.  (Rows in 4 bits, 8 experts, 2048 rows of 14336 columns each, 4096 outputs: 510 us, 3.8
+// PFLOP/s, on zeros 451; four wavefronts of 128 x 128, which read a third less from LDS, 541.)  Both operands go from memory straight to
+// LDS, as they are: rows of 128 bytes, which are 256 columns of codes (a superblock: eight blocks of 32, a 16-byte piece each) or 64
+// columns of BF16.  A load fills 1 KiB of LDS without gaps, so instead of padding, the lane that fills position p of a row fetches piece
+// p ^ ((row >> 1) & 7): 16 neighbouring rows' pieces of one number then lie in 64 different banks.
 // Which columns a matrix instruction's k numbers stand for is free as long as both operands agree.  Lanes 0..31 take the first half
 // of a superblock's blocks and lanes 32..63 the second, so that a lane's scales of a superblock are four neighbouring bytes.
 #include "mx_device.h"
