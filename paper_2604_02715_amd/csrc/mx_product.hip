@@ -307,10 +307,12 @@ __global__ __launch_bounds__(kThreads, 2) void mx_strip_kernel(MxProductArgs a, 
 // The gradient likewise.  A workgroup has 16 MI rows and 256 columns, its four or eight wavefronts share out the outputs, 32 at a time.
 // Lane (r, q) loads 16 neighbouring columns of eight outputs, eight bytes of each, turns them into sixteen fragments of eight outputs by a
 // conversion and a permutation to each two numbers, and fragment c goes to a matrix instruction whose results are column c of every lane's.
+// A wavefront waits for its loads, so what counts is how many there are: three to a SIMD with 16 rows, two with 32 (900 tokens of 512 experts,
+// 512 columns 163 -> 91 us, 100 tokens 47 -> 41; fetching the next outputs ahead, with fewer wavefronts, 98 and 52).
 template <int MI, int WAVES, bool VEC, typename OUT>
-__global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
+__global__ __launch_bounds__(64 * WAVES, MI == 1 && WAVES == 4 ? 3 : 2) void mx_stream_grad_kernel(MxProductArgs a, uint32_t strips, uint64_t items) {
     __shared__ uint32_t s_tile[kTileWords];
-    __shared__ f32x4 s_acc[WAVES - 1][16][64];
+    __shared__ f32x4 s_acc[WAVES - 1][8][64];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
     const uint32_t blocks = a.K / kMxBlock, chunks = (a.N + 31) / 32;
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -327,12 +329,16 @@ __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArg
             const uint64_t row = uint64_t(t.expert) * a.N + chunk * 32;
             const uint32_t left = min(a.N - chunk * 32, 32u);
             const row_t w = bytes_at(a.w, row * (a.K / 2), left * (a.K / 2)), ws = bytes_at(a.ws, row * blocks, left * blocks);
+            uint32_t w_at = column < a.K ? 8 * q * (a.K / 2) + column / 2 : kNowhere;
+            uint32_t s_at = column < a.K ? 8 * q * blocks + column / kMxBlock : kNowhere;
+            // (made anew for each chunk: kept for all of them, the sixteen places below cost a wavefront to a SIMD)
+            asm volatile("" : "+v"(w_at), "+v"(s_at));
             u32x2 codes[8];
             uint32_t scales[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                codes[j] = __builtin_amdgcn_raw_buffer_load_b64(w, column < a.K ? (8 * q + j) * (a.K / 2) + column / 2 : kNowhere, 0, kStream);
-                scales[j] = __builtin_amdgcn_raw_buffer_load_b8(ws, column < a.K ? (8 * q + j) * blocks + column / kMxBlock : kNowhere, 0, kCached);
+                codes[j] = __builtin_amdgcn_raw_buffer_load_b64(w, w_at + j * (a.K / 2), 0, kStream);
+                scales[j] = __builtin_amdgcn_raw_buffer_load_b8(ws, s_at + j * blocks, 0, kCached);
             }
             u32x4 x[MI];
             const uint32_t n = chunk * 32 + 8 * q;
@@ -377,20 +383,26 @@ __global__ __launch_bounds__(64 * WAVES) void mx_stream_grad_kernel(MxProductArg
                 }
             }
         }
-        // The wavefronts' sums in their order, 16 rows at a time; a lane then has 16 neighbouring columns of four lanes' for its row.
+        // The wavefronts' sums in their order, 16 rows at a time and half of the columns; a lane then has 16 neighbouring columns of four
+        // lanes' for its row.
 #pragma unroll
         for (int m = 0; m < MI; ++m) {
-            if (m) __syncthreads();
-            if (wave) {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) s_acc[wave - 1][c][lane] = acc[m][c];
+            for (int half = 0; half < 2; ++half) {
+                if (m || half) __syncthreads();
+                if (wave) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) s_acc[wave - 1][c][lane] = acc[m][half * 8 + c];
+                }
+                __syncthreads();
+                if (wave == 0) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+#pragma unroll
+                        for (int k = 0; k < WAVES - 1; ++k) acc[m][half * 8 + c] += s_acc[k][c][lane];
+                }
             }
-            __syncthreads();
             if (wave != 0 || m * 16 + r >= t.rows) continue;
-#pragma unroll
-            for (int c = 0; c < 16; ++c)
-#pragma unroll
-                for (int k = 0; k < WAVES - 1; ++k) acc[m][c] += s_acc[k][c][lane];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t k = k0 + (4 * q + i) * 16;
@@ -436,10 +448,10 @@ void go_stream(const MxProductArgs& a, hipStream_t stream) {
 template <int MI, bool VEC, typename OUT>
 void go_stream_grad(const MxProductArgs& a, hipStream_t stream) {
     const Plan p(a, 16 * MI, a.K, 256);
-    // Eight wavefronts where there are fewer than four workgroups for a CU: 160 experts, 13 rows each, 1536 columns 185 -> 162 us,
-    // 8 experts, 16 rows, 4096 columns of 28672 outputs 369 -> 217; with more workgroups the longer sum at the end costs more
-    // (512 experts, 512 columns 90 -> 95).
-    if (std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E)) * p.strips < 4 * 256)
+    // Eight wavefronts where there are fewer workgroups than CUs. Four / eight, us: 20 workgroups (one token of 512 experts, 512 columns)
+    // 15.9 / 13.7, 128 (8 experts, 16 rows, 4096 columns of 28672 outputs) 290 / 221, 448 (8 experts, 14336 columns, 4 rows) 66 / 71,
+    // 960 (160 experts, 1536 columns) 3 rows 140 / 137, 13 rows 149 / 165, 3200 (160 experts, 5120 columns, 13 rows) 283 / 329.
+    if (std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E)) * p.strips < 256)
         hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 8, VEC, OUT>), dim3(p.grid), dim3(512), 0, stream, a, p.strips, p.items);
     else
         hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 4, VEC, OUT>), dim3(p.grid), dim3(256), 0, stream, a, p.strips, p.items);
@@ -470,6 +482,9 @@ void pick_stream(const MxProductArgs& a, hipStream_t stream) {
 // Two 16-row tiles of rows to a workgroup from this many rows for each expert on, on average: some experts have more than 16 then, and
 // their weights are read once (8 experts of 16 rows, 4096 columns, 28672 outputs: 156 -> 133 us, rows in 4 bits 134 -> 111; 12.8 rows level).
 constexpr uint32_t kTwoTiles = 9;
+// and for the gradient, where they cost a wavefront to a SIMD (one / two, us: 512 experts, 10 rows, 2048 columns 149 / 164, 160 experts, 13 rows, 5120
+// columns 307 / 283, 512 experts, 17 rows 100 / 91, 20 rows 466 / 304)
+constexpr uint32_t kTwoTilesGrad = 12;
 
 // Workgroups of the wide tiles of `rows` rows that a call is expected to have: an expert's last tile is half full
 uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
@@ -516,7 +531,7 @@ hipError_t product_grad(const MxProductArgs& a, hipStream_t stream) {
     // tiles of 128, 1464 of 256.
     if (per_expert > (vec ? 32 : 128) && wide_workgroups(a, 128, a.K) >= 96 && mx_wide_grad_takes(a))
         return launch_mx_wide_grad(a, per_expert <= (vec ? 80 : 256) || wide_workgroups(a, 128, a.K) <= 256, sizeof(OUT) == 4, stream);
-    if (per_expert >= kTwoTiles) vec ? go_stream_grad<2, true, OUT>(a, stream) : go_stream_grad<2, false, OUT>(a, stream);
+    if (per_expert >= kTwoTilesGrad) vec ? go_stream_grad<2, true, OUT>(a, stream) : go_stream_grad<2, false, OUT>(a, stream);
     else vec ? go_stream_grad<1, true, OUT>(a, stream) : go_stream_grad<1, false, OUT>(a, stream);
     return hipGetLastError();
 }
