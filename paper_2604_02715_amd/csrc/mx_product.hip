@@ -496,9 +496,10 @@ uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
 //   rows           26               40               60               120             200
 //   4 bits         151 /  - / 207   159 /  - / 216   180 /  - / 224   279 /  - / 254  433 /  - / 311      (80: 246 / 234)
 //   BF16           171 / 215 / 278  235 / 252 / 288  292 / 269 / 308    - / 409 / 408   - / 631 / 558
-//   gradient       243 / 273 / 346  394 / 288 / 355  537 / 356 / 386    - / 504 / 447   - / 788 / 568
+//   gradient       197 / 276 / 346  303 / 293 / 355  379 / 354 / 386    - / 504 / 447   - / 788 / 568  (35: 279 / 291)
 // and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns 152 / 186 / 207 with BF16 rows; of 256
-// columns, 1024 outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 /  - / 31.  Tiles of 128 rows also where those of
+// columns, 1024 outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 /  - / 31, of 28672 outputs
+// and 4096 columns 40 rows 256 / 305 /  - , 56 rows 303 / 334 /  - , 64 rows 453 / 392 /  - .  Tiles of 128 rows also where those of
 // 256 would be two rounds or three with the last one far from full (BF16, 128 / 256; same layer: 512 rows 522 / 625, 700 rows 580 / 654,
 // 1000 rows 845 / 910; 28672 outputs, 300 rows 587 / 541), for the gradient where they are one round (28672 outputs of 4096 columns:
 // 150 rows 430 / 540, 300 rows 868 / 612).
@@ -527,10 +528,11 @@ template <typename OUT>
 hipError_t product_grad(const MxProductArgs& a, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
     const bool vec = a.rows_vec && a.N % 8 == 0;
-    // Rows through registers make longer steps: 160 experts of 5119 outputs, 40 rows each, streamed 422, wide 820; 90 rows 752; 110 rows 1177 in
-    // tiles of 128, 1464 of 256.
-    if (per_expert > (vec ? 32 : 128) && wide_workgroups(a, 128, a.K) >= 96 && mx_wide_grad_takes(a))
-        return launch_mx_wide_grad(a, per_expert <= (vec ? 80 : 256) || wide_workgroups(a, 128, a.K) <= 256, sizeof(OUT) == 4, stream);
+    // Rows through registers make longer steps, streamed / wide: 160 experts of 5119 outputs and 1536 columns, 100 rows each 704 / 985, 260 rows
+    // 1644 / 2390, 400 rows 2470 / 3108; 8 experts of 4095 outputs and 14336 columns, 100 rows 301 / 298, 200 rows 540 / 543, 260 rows 688 / 675,
+    // 400 rows 1020 / 844.
+    if (per_expert > (vec ? 32 : 256) && wide_workgroups(a, 128, a.K) >= 128 && mx_wide_grad_takes(a))
+        return launch_mx_wide_grad(a, (vec && per_expert <= 80) || wide_workgroups(a, 128, a.K) <= 256, sizeof(OUT) == 4, stream);
     if (per_expert >= kTwoTilesGrad) vec ? go_stream_grad<2, true, OUT>(a, stream) : go_stream_grad<2, false, OUT>(a, stream);
     else vec ? go_stream_grad<1, true, OUT>(a, stream) : go_stream_grad<1, false, OUT>(a, stream);
     return hipGetLastError();

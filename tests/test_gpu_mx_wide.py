@@ -93,6 +93,19 @@ def test_gradient_rows_anywhere(counts, K, N, gap, shift):
     gradient(counts, N, K, BF16, gap, shift)
 
 
+@pytest.mark.parametrize("counts,K", [([600] * 3, 4096), ([700, 0, 513, 130], 3968), ([300, 0, 513, 600], 16384)])
+@pytest.mark.parametrize("N,gap,shift", [(8, 1, 0), (9, 0, 0), (250, 6, 0), (257, 7, 0), (264, 0, 3), (264, 0, 0), (1027, 5, 2)])
+def test_gradient_rows_anywhere_of_many_rows(counts, K, N, gap, shift):
+    gradient(counts, N, K, BF16, gap, shift)
+
+
+@pytest.mark.parametrize("out_type", [BF16, F32])
+@pytest.mark.parametrize("counts,K", [([257, 2, 255], 6912), ([70] * 5, 8200 // 32 * 32)])
+@pytest.mark.parametrize("N", [8, 264, 1048])
+def test_gradient_few_tiles(counts, K, N, out_type):
+    gradient(counts, N, K, out_type)
+
+
 @pytest.mark.parametrize("counts,N", [(FEW, 16390), (MANY, 33000)])
 @pytest.mark.parametrize("gap", [0, 1])
 def test_nan_stays_with_its_row(counts, N, gap):
@@ -120,8 +133,16 @@ def test_nan_stays_with_its_row(counts, N, gap):
 @pytest.mark.parametrize("counts", [FEW, MANY])
 @pytest.mark.parametrize("N,gap", [(264, 0), (261, 0)])
 def test_gradient_nan_stays_with_its_row(counts, N, gap):
+    gradient_nan(counts, N, 16416)
+
+
+@pytest.mark.parametrize("K", [3968, 16416])
+def test_gradient_nan_stays_with_its_row_of_many_rows(K):
+    gradient_nan([700, 513, 0, 130], 261, K)
+
+
+def gradient_nan(counts, N, K):
     offsets, n_rows, n = plain.groups(counts, align=4, ahead=2)
-    K = 16416
     wc, ws = plain.random_weights(4, N, K, 6)
     d = torch.randn(n, N, device="cuda").to(BF16)
     clean, back = torch.full((n, K), 7.0, device="cuda"), torch.full((n, K), 7.0, device="cuda")
