@@ -499,10 +499,10 @@ uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
 //   gradient       197 / 276 / 346  303 / 293 / 355  379 / 354 / 386    - / 504 / 447   - / 788 / 568  (35: 279 / 291)
 // and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns 152 / 186 / 207 with BF16 rows; of 256
 // columns, 1024 outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 /  - / 31, of 28672 outputs
-// and 4096 columns 40 rows 256 / 305 /  - , 56 rows 303 / 334 /  - , 64 rows 453 / 392 /  - .  Tiles of 128 rows also where those of
-// 256 would be two rounds or three with the last one far from full (BF16, 128 / 256; same layer: 512 rows 522 / 625, 700 rows 580 / 654,
-// 1000 rows 845 / 910; 28672 outputs, 300 rows 587 / 541), for the gradient where they are one round (28672 outputs of 4096 columns:
-// 150 rows 430 / 540, 300 rows 868 / 612).
+// and 4096 columns 40 rows 256 / 305 /  - , 56 rows 303 / 334 /  - , 64 rows 453 / 392 /  - .  Tiles of 128 rows
+// also where those of 256 would be two rounds with the last one far from full (BF16, 128 / 256; same layer: 512 rows 527 / 598, 700 rows
+// 591 / 620, 1000 rows 877 / 869; 28672 outputs, 300 rows 595 / 551), for the gradient where they are one round (28672 outputs of 4096
+// columns: 150 rows 447 / 478, 300 rows 877 / 630).
 template <typename OUT>
 hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
     const uint32_t per_expert = a.cap / a.E;
@@ -515,7 +515,7 @@ hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
         else pick_stream<1, true, OUT>(a, stream);
     } else {
         if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 176 && mx_wide_takes(a, false))
-            return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 640, sizeof(OUT) == 4, stream);
+            return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 512, sizeof(OUT) == 4, stream);
         if (!a.rows_vec || !near_rows(a, false)) go_stream<2, 4, false, false, OUT>(a, stream);
         else if (per_expert > 32) pick_stream<4, false, OUT>(a, stream);
         else if (per_expert >= kTwoTiles) pick_stream<2, false, OUT>(a, stream);
