@@ -5,6 +5,8 @@
 // code's 0 .. 6; each number over 2^e goes to its nearest code, ties to the even one, and past 6 to 6.  The largest is found
 // on the bits (as integers they have the magnitudes' order, NaN on top), and e is its exponent field less 2: nothing is rounded
 // but the number itself, once, in v_cvt_scalef32_pk_fp4_*, which does scale, rounding and saturation of two.
+#include <type_traits>
+
 #include "block_device.h"
 #include "mx_ops.h"
 
@@ -214,12 +216,15 @@ struct Piece {
     }
 };
 
+// e^x as a power of 2: 1 / ln 2 in two parts, the second, and what the first rounds off, multiplied on behind the power
+constexpr float kLog2E = 0x1.715476p+0f, kLog2ELow = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
+
 // p = 1 / (1 + e^-g) and q = 1 - p, both from t = e^-|g| <= 1, the smaller one as t / (1 + t): neither overflows or is a difference of rounded
-// numbers.  The power is that of 2 of the product with 1 / ln 2 in two parts, what the first rounds off multiplied on behind it; the
-// quotient one Newton step on the hardware's reciprocal.  Both good to 2 ulp (0 below e^-87), with half of expf's and the division's
-// instructions, of which there were more than memory leaves time for (4097 x 14336 BF16 69 us).
+// numbers.  The power is the hardware's of 2, the quotient one Newton step on its reciprocal.  Both good to 2 ulp, with half of expf's and the
+// division's instructions, of which there were more than memory leaves time for (4097 x 14336 BF16 69 us).  t is 0 where it would be below the
+// normal numbers: gates below kFar are not for this.
+constexpr float kFar = -87.0f;
 __device__ __forceinline__ void sigmoids(float g, float& p, float& q) {
-    constexpr float kLog2E = 0x1.715476p+0f, kLog2ELow = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
     const float x = -fminf(fabsf(g), 200.0f), y = x * kLog2E, low = fmaf(x, kLog2ELow, fmaf(x, kLog2E, -y));
     float t = __builtin_amdgcn_exp2f(y);
     t = fmaf(t, low * kLn2, t);
@@ -229,6 +234,21 @@ __device__ __forceinline__ void sigmoids(float g, float& p, float& q) {
     const float s = t * r;
     p = g >= 0.0f ? r : s;
     q = g >= 0.0f ? s : r;
+}
+
+// p for gates below kFar, where it is e^g to more digits than are kept.  It may be far below FP32's numbers and h, or a gradient, not: what
+// it is multiplied by is in 64 bits, too, and rounded behind the last product.
+__device__ __forceinline__ double far_sigmoid(float g) {
+    const float x = fmaxf(g, -2000.0f), whole = rintf(x * kLog2E), t = __builtin_amdgcn_exp2f(fmaf(x, kLog2E, -whole));
+    return __builtin_amdgcn_ldexp(double(fmaf(t, x * kLog2ELow * kLn2, t)), int(whole));
+}
+__device__ __forceinline__ bool is_far(float g) { return g < kFar && g > -INFINITY; }    // (of minus infinity all is NaN, as written)
+template <int N>
+__device__ __forceinline__ bool any_far(const float (&g)[N]) {
+    float least = g[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) least = fminf(least, g[j]);
+    return least < kFar;
 }
 
 // h = g / (1 + e^-g) u
@@ -247,6 +267,11 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(SwigluArgs a, Shares s
             float p, q;
             sigmoids(g.f[j], p, q);
             h.f[j] = g.f[j] * p * u.f[j];
+        }
+        if (any_far(g.f)) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (is_far(g.f[j])) h.f[j] = float(double(g.f[j]) * far_sigmoid(g.f[j]) * double(u.f[j]));
         }
         h.store(static_cast<H*>(a.out) + s.row * a.out_stride + s.piece * N);
     }
@@ -273,13 +298,23 @@ __global__ __launch_bounds__(kThreads) void swiglu_grad_kernel(SwigluArgs a, Sha
         for (int u = 0; u < kAtOnce; ++u) {
             if (!share[u].valid) continue;
             Piece<T, N> dg, du;
+            auto derive = [&](auto FAR) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                float p, q;
-                sigmoids(g[u].f[j], p, q);
-                du.f[j] = d[u].f[j] * (g[u].f[j] * p);
-                dg.f[j] = d[u].f[j] * up[u].f[j] * (p * fmaf(g[u].f[j], q, 1.0f));
-            }
+                for (int j = 0; j < N; ++j) {
+                    float p, q;
+                    sigmoids(g[u].f[j], p, q);
+                    du.f[j] = d[u].f[j] * (g[u].f[j] * p);
+                    dg.f[j] = d[u].f[j] * up[u].f[j] * (p * fmaf(g[u].f[j], q, 1.0f));
+                    if (decltype(FAR)::value && is_far(g[u].f[j])) {
+                        const double gate = double(g[u].f[j]), dp = far_sigmoid(g[u].f[j]) * double(d[u].f[j]);
+                        du.f[j] = float(gate * dp);
+                        dg.f[j] = float((1.0 + gate) * dp * double(up[u].f[j]));
+                    }
+                }
+            };
+            // two bodies for the whole wavefront: with a branch behind one (BF16, 4097 x 14336) 97 -> 104 us, so 97 -> 100
+            if (__any(any_far(g[u].f))) derive(std::true_type{});
+            else derive(std::false_type{});
             T* out = static_cast<T*>(a.out) + share[u].row * a.out_stride + share[u].piece * N;
             dg.store(out);
             du.store(out + a.F);
