@@ -5,6 +5,8 @@
 
 #include <cstdint>
 
+#include "mx_plan.h"
+
 namespace fluxmoe {
 
 constexpr uint32_t kMxBlock = 32;            // columns that share a scale
@@ -51,11 +53,9 @@ struct MxProductArgs {
     uint32_t out_vec;            // out's rows at 16-byte addresses
 };
 hipError_t launch_mx_product(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream);
-// Tiles of 256 x 256, or with `half` (BF16 rows) of 128 rows (mx_tiles.hip)
-bool mx_wide_takes(const MxProductArgs& a, bool mx_rows);
-hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool half, bool out_f32, hipStream_t stream);
-bool mx_wide_grad_takes(const MxProductArgs& a);
-hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool half, bool out_f32, hipStream_t stream);
+// Wide tiles, as chosen (mx_tiles.hip)
+hipError_t launch_mx_wide(const MxProductArgs& a, const MxChoice& choice, bool mx_rows, bool out_f32, hipStream_t stream);
+hipError_t launch_mx_wide_grad(const MxProductArgs& a, const MxChoice& choice, bool out_f32, hipStream_t stream);
 hipError_t launch_mx_product_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream);
 
 }  // namespace fluxmoe

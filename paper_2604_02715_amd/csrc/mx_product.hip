@@ -7,8 +7,6 @@
 // rows in the BF16 matrix instructions; rows in 4 bits themselves go to the scaled ones as they are.  Sums are FP32.
 //
 // Which rows are whose is known on the device only: a workgroup adds up the experts' tiles and finds its own (find_tile).
-#include <algorithm>
-
 #include "mx_device.h"
 
 namespace fluxmoe {
@@ -415,133 +413,77 @@ __global__ __launch_bounds__(64 * WAVES, MI == 1 && WAVES == 4 ? 3 : 2) void mx_
     }
 }
 
-// Tiles that the groups can have: full ones and one unfinished one for each expert that has rows.
-uint64_t most_tiles(const MxProductArgs& a, uint32_t size) { return a.cap / size + (a.cap < a.E ? a.cap : a.E); }
-
-struct Plan {
+struct Grid {
     uint32_t strips;
     uint64_t items;
-    uint32_t grid;
-    Plan(const MxProductArgs& a, uint32_t rows, uint32_t outs, uint32_t width) {
+    uint32_t workgroups;
+    Grid(const MxCall& c, uint32_t rows, uint32_t outs, uint32_t width) {
         strips = (outs + width - 1) / width;
-        items = most_tiles(a, rows) * strips;
-        grid = uint32_t(items < kMaxGrid ? items : kMaxGrid);
+        items = mx_most_tiles(c, rows) * strips;
+        workgroups = uint32_t(items < kMaxGrid ? items : kMaxGrid);
     }
 };
 
-// Scales of the weights and of rows in 4 bits, four at a time, at addresses of words
-template <bool MX>
-bool whole_scales(const MxProductArgs& a) {
+MxCall call_of(const MxProductArgs& a, bool mx_rows) {
     const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
-    return words(a.ws, a.K / kMxBlock) && (!MX || words(a.row_scales, a.row_scales_stride));
+    return {a.cap, a.E, a.N, a.K, a.row_stride, a.row_scales_stride, mx_rows, a.rows_vec != 0, words(a.ws, a.K / kMxBlock),
+            words(a.row_scales, a.row_scales_stride)};
 }
-// 64 rows' places, counted from the first one's, within 31 bits
-bool near_rows(const MxProductArgs& a, bool mx_rows) { return a.row_stride < (1u << 24) && (!mx_rows || a.row_scales_stride < (1u << 24)); }
+
 template <int MI, int NI, bool MX, bool VEC, typename OUT>
-void go_stream(const MxProductArgs& a, hipStream_t stream) {
-    const Plan p(a, 16 * MI, a.N, 16 * NI);
-    if (VEC && whole_scales<MX>(a))
-        hipLaunchKernelGGL((mx_stream_kernel<MI, NI, MX, VEC, VEC, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
-    else
-        hipLaunchKernelGGL((mx_stream_kernel<MI, NI, MX, VEC, false, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+void go_stream(const MxProductArgs& a, const MxCall& c, bool whole, hipStream_t stream) {
+    const Grid g(c, 16 * MI, a.N, 16 * NI);
+    if (VEC && whole) hipLaunchKernelGGL((mx_stream_kernel<MI, NI, MX, VEC, VEC, OUT>), dim3(g.workgroups), dim3(kThreads), 0, stream, a, g.strips, g.items);
+    else hipLaunchKernelGGL((mx_stream_kernel<MI, NI, MX, VEC, false, OUT>), dim3(g.workgroups), dim3(kThreads), 0, stream, a, g.strips, g.items);
+}
+template <int MI, bool MX, typename OUT>
+void go_strip(const MxProductArgs& a, const MxCall& c, bool whole, hipStream_t stream) {
+    constexpr int NI = mx_strip_outs(MX, 16 * MI) / 16;
+    const Grid g(c, 16 * MI, a.N, 64 * NI);
+    if (whole) hipLaunchKernelGGL((mx_strip_kernel<MI, NI, MX, true, OUT>), dim3(g.workgroups), dim3(kThreads), 0, stream, a, g.strips, g.items);
+    else hipLaunchKernelGGL((mx_strip_kernel<MI, NI, MX, false, OUT>), dim3(g.workgroups), dim3(kThreads), 0, stream, a, g.strips, g.items);
 }
 template <int MI, bool VEC, typename OUT>
-void go_stream_grad(const MxProductArgs& a, hipStream_t stream) {
-    const Plan p(a, 16 * MI, a.K, 256);
-    // Eight wavefronts where there are fewer workgroups than CUs. Four / eight, us: 20 workgroups (one token of 512 experts, 512 columns)
-    // 15.9 / 13.7, 128 (8 experts, 16 rows, 4096 columns of 28672 outputs) 290 / 221, 448 (8 experts, 14336 columns, 4 rows) 66 / 71,
-    // 960 (160 experts, 1536 columns) 3 rows 140 / 137, 13 rows 149 / 165, 3200 (160 experts, 5120 columns, 13 rows) 283 / 329.
-    if (std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E)) * p.strips < 256)
-        hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 8, VEC, OUT>), dim3(p.grid), dim3(512), 0, stream, a, p.strips, p.items);
-    else
-        hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 4, VEC, OUT>), dim3(p.grid), dim3(256), 0, stream, a, p.strips, p.items);
-}
-template <int MI, int NI, bool MX, typename OUT>
-void go_strip(const MxProductArgs& a, bool whole, hipStream_t stream) {
-    const Plan p(a, 16 * MI, a.N, 64 * NI);
-    if (whole) hipLaunchKernelGGL((mx_strip_kernel<MI, NI, MX, true, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
-    else hipLaunchKernelGGL((mx_strip_kernel<MI, NI, MX, false, OUT>), dim3(p.grid), dim3(kThreads), 0, stream, a, p.strips, p.items);
+void go_stream_grad(const MxProductArgs& a, const MxCall& c, uint32_t waves, hipStream_t stream) {
+    const Grid g(c, 16 * MI, a.K, 256);
+    if (waves == 8) hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 8, VEC, OUT>), dim3(g.workgroups), dim3(512), 0, stream, a, g.strips, g.items);
+    else hipLaunchKernelGGL((mx_stream_grad_kernel<MI, 4, VEC, OUT>), dim3(g.workgroups), dim3(256), 0, stream, a, g.strips, g.items);
 }
 
-// Which of the three. Times in us, 16-bit outputs, even routing but for 512 experts:
-//   rows in 4 bits, side by side / quarters: 512 columns (512 experts, 900 tokens) 88 / 203, 1536 (160, 256) 143 / 167,
-//   2048 (512, 256) 100 / 106, 4096 (8, 64) 154 / 134, 5120 (160, 16) 151 / 116: long rows are better read a whole piece at a time, and
-//   there are more workgroups;
-//   BF16 rows, which quarters fetch for every 64 outputs: 1536 (160, 256) 153 / 253, 5120 (160, 16) 145 / 156;
-//   BF16 rows, 32 / 64 outputs to a wavefront: one tile of rows 153 / 159 (1536), 145 / 155 (5120), two 176 / 171.
-// Where the workgroups would be few, narrow ones with a quarter each (one token of 512 experts, 2048 columns, 1024 outputs 7.7).
-template <int MI, bool MX, typename OUT>
-void pick_stream(const MxProductArgs& a, hipStream_t stream) {
-    const uint64_t tiles = std::max<uint64_t>(a.cap / (16 * MI), std::min(a.cap, a.E));
-    constexpr int kStrip = MX || MI == 2 ? 4 : 2;            // sixteens of outputs to a wavefront
-    if constexpr (MI == 4) go_strip<MI, kStrip, MX, OUT>(a, whole_scales<MX>(a), stream);
-    else if ((!MX || a.K <= 2048) && tiles * (a.N / (64 * kStrip)) >= 448) go_strip<MI, kStrip, MX, OUT>(a, whole_scales<MX>(a), stream);
-    else if (tiles * (a.N / 64) >= 512) go_stream<MI, 4, MX, true, OUT>(a, stream);
-    else go_stream<MI, 1, MX, true, OUT>(a, stream);
-}
-// Two 16-row tiles of rows to a workgroup from this many rows for each expert on, on average: some experts have more than 16 then, and
-// their weights are read once (8 experts of 16 rows, 4096 columns, 28672 outputs: 156 -> 133 us, rows in 4 bits 134 -> 111; 12.8 rows level).
-constexpr uint32_t kTwoTiles = 9;
-// and for the gradient, where they cost a wavefront to a SIMD (one / two, us: 512 experts, 10 rows, 2048 columns 149 / 164, 160 experts, 13 rows, 5120
-// columns 307 / 283, 512 experts, 17 rows 100 / 91, 20 rows 466 / 304)
-constexpr uint32_t kTwoTilesGrad = 12;
-
-// Workgroups of the wide tiles of `rows` rows that a call is expected to have: an expert's last tile is half full
-uint64_t wide_workgroups(const MxProductArgs& a, uint32_t rows, uint32_t outs) {
-    return (a.cap / rows + std::min(a.cap, a.E) / 2) * ((uint64_t(outs) + 255) / 256);
-}
-
-// The wide tiles take over where the matrix cores bound the call, by the rows to an expert on average. Times in us, streamed / wide tiles
-// of 128 rows / of 256, 160 experts of 1536 columns and 5120 outputs (and turned round for the gradient):
-//   rows           26               40               60               120             200
-//   4 bits         151 /  - / 207   159 /  - / 216   180 /  - / 224   279 /  - / 254  433 /  - / 311      (80: 246 / 234)
-//   BF16           171 / 215 / 278  235 / 252 / 288  292 / 269 / 308    - / 409 / 408   - / 631 / 558
-//   gradient       197 / 276 / 346  303 / 293 / 355  379 / 354 / 386    - / 504 / 447   - / 788 / 568  (35: 279 / 291)
-// and where they are enough for the CUs: 8 experts, 96 rows, 4096 outputs of 14336 columns 152 / 186 / 207 with BF16 rows; of 256
-// columns, 1024 outputs 256 rows in 4 bits 8.3 /  - / 12.1, the gradient of 1024 rows 24 /  - / 31, of 28672 outputs
-// and 4096 columns 40 rows 256 / 305 /  - , 56 rows 303 / 334 /  - , 64 rows 453 / 392 /  - .  Tiles of 128 rows
-// also where those of 256 would be two rounds with the last one far from full (BF16, 128 / 256; same layer: 512 rows 527 / 598, 700 rows
-// 591 / 620, 1000 rows 877 / 869; 28672 outputs, 300 rows 595 / 551), for the gradient where they are one round (28672 outputs of 4096
-// columns: 150 rows 447 / 478, 300 rows 877 / 630).
-template <typename OUT>
-hipError_t product(const MxProductArgs& a, bool mx_rows, hipStream_t stream) {
-    const uint32_t per_expert = a.cap / a.E;
-    if (mx_rows) {
-        if (per_expert > 64 && wide_workgroups(a, 256, a.N) >= 96 && mx_wide_takes(a, true))
-            return launch_mx_wide(a, true, false, sizeof(OUT) == 4, stream);
-        if (!a.rows_vec || !near_rows(a, true)) go_stream<2, 4, true, false, OUT>(a, stream);
-        else if (per_expert > 32) pick_stream<4, true, OUT>(a, stream);
-        else if (per_expert >= kTwoTiles) pick_stream<2, true, OUT>(a, stream);
-        else pick_stream<1, true, OUT>(a, stream);
+template <bool MX, typename OUT>
+hipError_t product(const MxProductArgs& a, hipStream_t stream) {
+    const MxCall c = call_of(a, MX);
+    const MxChoice k = mx_choose_product(c);
+    if (k.kernel == kMxWide) return launch_mx_wide(a, k, MX, sizeof(OUT) == 4, stream);
+    if (k.kernel == kMxStrip) {
+        if (k.rows == 64) go_strip<4, MX, OUT>(a, c, k.whole, stream);
+        else if (k.rows == 32) go_strip<2, MX, OUT>(a, c, k.whole, stream);
+        else go_strip<1, MX, OUT>(a, c, k.whole, stream);
+    } else if (!k.vec) {
+        go_stream<2, 4, MX, false, OUT>(a, c, false, stream);
+    } else if (k.rows == 32) {
+        k.outs == 64 ? go_stream<2, 4, MX, true, OUT>(a, c, k.whole, stream) : go_stream<2, 1, MX, true, OUT>(a, c, k.whole, stream);
     } else {
-        if (per_expert > 48 && wide_workgroups(a, 128, a.N) >= 176 && mx_wide_takes(a, false))
-            return launch_mx_wide(a, false, per_expert <= 112 || wide_workgroups(a, 256, a.N) < 512, sizeof(OUT) == 4, stream);
-        if (!a.rows_vec || !near_rows(a, false)) go_stream<2, 4, false, false, OUT>(a, stream);
-        else if (per_expert > 32) pick_stream<4, false, OUT>(a, stream);
-        else if (per_expert >= kTwoTiles) pick_stream<2, false, OUT>(a, stream);
-        else pick_stream<1, false, OUT>(a, stream);
+        k.outs == 64 ? go_stream<1, 4, MX, true, OUT>(a, c, k.whole, stream) : go_stream<1, 1, MX, true, OUT>(a, c, k.whole, stream);
     }
     return hipGetLastError();
 }
 
 template <typename OUT>
 hipError_t product_grad(const MxProductArgs& a, hipStream_t stream) {
-    const uint32_t per_expert = a.cap / a.E;
-    const bool vec = a.rows_vec && a.N % 8 == 0;
-    // Rows through registers make longer steps, streamed / wide: 160 experts of 5119 outputs and 1536 columns, 100 rows each 704 / 985, 260 rows
-    // 1644 / 2390, 400 rows 2470 / 3108; 8 experts of 4095 outputs and 14336 columns, 100 rows 301 / 298, 200 rows 540 / 543, 260 rows 688 / 675,
-    // 400 rows 1020 / 844.
-    if (per_expert > (vec ? 32 : 256) && wide_workgroups(a, 128, a.K) >= 128 && mx_wide_grad_takes(a))
-        return launch_mx_wide_grad(a, (vec && per_expert <= 80) || wide_workgroups(a, 128, a.K) <= 256, sizeof(OUT) == 4, stream);
-    if (per_expert >= kTwoTilesGrad) vec ? go_stream_grad<2, true, OUT>(a, stream) : go_stream_grad<2, false, OUT>(a, stream);
-    else vec ? go_stream_grad<1, true, OUT>(a, stream) : go_stream_grad<1, false, OUT>(a, stream);
+    const MxCall c = call_of(a, false);
+    const MxChoice k = mx_choose_grad(c);
+    if (k.kernel == kMxWide) return launch_mx_wide_grad(a, k, sizeof(OUT) == 4, stream);
+    if (k.rows == 32) k.vec ? go_stream_grad<2, true, OUT>(a, c, k.waves, stream) : go_stream_grad<2, false, OUT>(a, c, k.waves, stream);
+    else k.vec ? go_stream_grad<1, true, OUT>(a, c, k.waves, stream) : go_stream_grad<1, false, OUT>(a, c, k.waves, stream);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_mx_product(const MxProductArgs& a, bool mx_rows, bool out_f32, hipStream_t stream) {
-    return out_f32 ? product<float>(a, mx_rows, stream) : product<bf16_t>(a, mx_rows, stream);
+    if (mx_rows) return out_f32 ? product<true, float>(a, stream) : product<true, bf16_t>(a, stream);
+    return out_f32 ? product<false, float>(a, stream) : product<false, bf16_t>(a, stream);
 }
 hipError_t launch_mx_product_grad(const MxProductArgs& a, bool out_f32, hipStream_t stream) {
     return out_f32 ? product_grad<float>(a, stream) : product_grad<bf16_t>(a, stream);

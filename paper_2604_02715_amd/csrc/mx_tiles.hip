@@ -13,7 +13,7 @@
 namespace fluxmoe {
 namespace {
 
-constexpr uint32_t kTile = 256;
+constexpr uint32_t kTile = kMxWideOuts;
 constexpr int kStage = 32768;                            // 256 rows of 128 bytes
 constexpr uint32_t kThreads = 512;
 constexpr uint32_t kScaleRow = 260;                      // words between the gradient's scales of two blocks of columns: in different banks
@@ -654,46 +654,33 @@ __global__ __launch_bounds__(kThreads) void mx_wide_kernel(MxProductArgs a, Wide
 }
 
 template <Mode MODE, int RT, typename OUT>
-void go(const MxProductArgs& a, bool vec, hipStream_t stream) {
+void go(const MxProductArgs& a, const MxChoice& choice, hipStream_t stream) {
     const WideGrid grid(a, 128 * RT, MODE == kGradRows ? a.K : a.N);
-    const auto words = [](const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 4 == 0; };
-    const bool whole = words(a.ws, a.K / kMxBlock) && (MODE != kMxRows || words(a.row_scales, a.row_scales_stride));
     const dim3 wgs(grid.total), threads(kThreads);
     constexpr uint32_t lds = 4 * kStage + scale_bytes(MODE) + 4 * kTileWords;
     if constexpr (MODE == kGradRows || (MODE == kBf16Rows && RT == 1)) {
-        if (!vec) {
+        if (!choice.vec) {
             hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, false, false, OUT>), wgs, threads, lds, stream, a, grid);
             return;
         }
     }
-    if (whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, true, true, OUT>), wgs, threads, lds, stream, a, grid);
+    if (choice.whole) hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, true, true, OUT>), wgs, threads, lds, stream, a, grid);
     else hipLaunchKernelGGL((mx_wide_kernel<MODE, RT, false, true, OUT>), wgs, threads, lds, stream, a, grid);
 }
 template <Mode MODE, int RT>
-hipError_t go(const MxProductArgs& a, bool vec, bool out_f32, hipStream_t stream) {
-    out_f32 ? go<MODE, RT, float>(a, vec, stream) : go<MODE, RT, bf16_t>(a, vec, stream);
+hipError_t go(const MxProductArgs& a, const MxChoice& choice, bool out_f32, hipStream_t stream) {
+    out_f32 ? go<MODE, RT, float>(a, choice, stream) : go<MODE, RT, bf16_t>(a, choice, stream);
     return hipGetLastError();
-}
-
-bool fits(const MxProductArgs& a, uint32_t outs) {           // places within 31 bits, and a launch of less than 2^31 threads
-    return a.row_stride < (1u << 23) && (a.cap / 128 + (a.cap < a.E ? a.cap : a.E)) * ((uint64_t(outs) + kTile - 1) / kTile + 8) < (1u << 21);
 }
 
 }  // namespace
 
-bool mx_wide_takes(const MxProductArgs& a, bool mx_rows) {
-    return fits(a, a.N) && (!mx_rows || (a.rows_vec && a.row_scales_stride < (1u << 22)));
+hipError_t launch_mx_wide(const MxProductArgs& a, const MxChoice& choice, bool mx_rows, bool out_f32, hipStream_t stream) {
+    if (mx_rows) return go<kMxRows, 2>(a, choice, out_f32, stream);
+    return choice.rows == 128 ? go<kBf16Rows, 1>(a, choice, out_f32, stream) : go<kBf16Rows, 2>(a, choice, out_f32, stream);
 }
-hipError_t launch_mx_wide(const MxProductArgs& a, bool mx_rows, bool half, bool out_f32, hipStream_t stream) {
-    if (mx_rows) return go<kMxRows, 2>(a, true, out_f32, stream);
-    // (256 rows that come through registers are more than there are)
-    return half || !a.rows_vec ? go<kBf16Rows, 1>(a, a.rows_vec, out_f32, stream) : go<kBf16Rows, 2>(a, true, out_f32, stream);
-}
-
-bool mx_wide_grad_takes(const MxProductArgs& a) { return fits(a, a.K) && a.N >= 8; }
-hipError_t launch_mx_wide_grad(const MxProductArgs& a, bool half, bool out_f32, hipStream_t stream) {
-    const bool vec = a.rows_vec && a.N % 8 == 0;
-    return half ? go<kGradRows, 1>(a, vec, out_f32, stream) : go<kGradRows, 2>(a, vec, out_f32, stream);
+hipError_t launch_mx_wide_grad(const MxProductArgs& a, const MxChoice& choice, bool out_f32, hipStream_t stream) {
+    return choice.rows == 128 ? go<kGradRows, 1>(a, choice, out_f32, stream) : go<kGradRows, 2>(a, choice, out_f32, stream);
 }
 
 }  // namespace fluxmoe
