@@ -141,3 +141,21 @@ def test_counts_that_do_not_fit_the_matrix(c):
     done = torch.zeros(n + 600, dtype=torch.bool, device="cuda")
     done[300:302], done[300 + n - 3:300 + n] = True, True
     assert bool((whole[~done] == 7.0).all()) and not bool((whole[done] == 7.0).all(dim=1).any())
+
+
+@pytest.mark.parametrize("out_type", [BF16, F32])
+@pytest.mark.parametrize("gap,shift", [(1, 0), (0, 1), (8, 0)])
+@pytest.mark.parametrize("c", ALIKE, ids=M.name)
+def test_outputs_at_any_stride(c, gap, shift, out_type):
+    """the kernel is the same wherever its outputs go, and so are their bits; what lies between rows is left"""
+    call = Call(c)
+    want = call.run(out_type)
+    whole = torch.full((want.shape[0] * (call.width + gap) + shift,), 7.0, dtype=out_type, device="cuda")
+    out = whole[shift:].view(want.shape[0], call.width + gap)[:, :call.width]
+    if call.grad:
+        X.product_grad(call.rows, call.offsets, call.counts, call.wc, call.ws, out)
+    else:
+        X.product(call.rows, call.offsets, call.counts, call.wc, call.ws, out, row_scales=call.scales)
+    assert torch.equal(out, want)
+    out.fill_(7.0)
+    assert bool((whole == 7.0).all())
