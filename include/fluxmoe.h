@@ -588,8 +588,9 @@ int fluxmoe_mx_dequantize(const uint8_t* codes, uint64_t codes_stride, const uin
  *            expert; E <= 4096, N <= 2^20
  *   rows     rows_type FLUXMOE_BF16 [rows_cap][K], or FLUXMOE_MXFP4: codes with row_scales [rows_cap][K / 32]
  *   out      out_type FLUXMOE_BF16 or FLUXMOE_F32 [rows_cap][N], not overlapping the rows; sums are FP32 and rounded once
- * Strides are in elements (codes and scales: bytes) from one row to the next; 0: the row's width.  Rows at other than
- * 16-byte addresses, for the gradient also with N not a multiple of 8, take slower kernels.
+ * Strides are in elements (codes and scales: bytes) from one row to the next; 0: the row's width.
+ * With BF16 rows, and in the gradient, a weight counts as BF16: 4 and 6 at scale 253, and from 2 on at 254, are infinite
+ * there.  Rows in 4 bits meet every weight as it is.
  */
 typedef struct {
     uint32_t E, N, K;
