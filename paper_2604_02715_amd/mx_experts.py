@@ -80,7 +80,7 @@ def _experts(offsets, counts, w_codes, w_scales, device):
 def product(rows, offsets, counts, w_codes, w_scales, out, *, row_scales=None, stream=None):
     """out [n][N] (bfloat16 or float32) <- rows times their expert's weights: rows bfloat16 [n][K], or uint8 codes [n][K / 2] with
     row_scales [n][K / 32]; offsets, counts as sort_tokens gives them; w_codes [E][N][K / 2], w_scales [E][N][K / 32].  Rows of no
-    expert are left as they are in out."""
+    expert are left as they are in out; many of them, as a large `align` of the sort leaves, cost time, and so does K no multiple of 128."""
     device = _place(rows, "rows")
     E, N, K = _experts(offsets, counts, w_codes, w_scales, device)
     n = rows.shape[0]
